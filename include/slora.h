@@ -362,6 +362,149 @@ int32_t slora_lora_shrink_expand(slora_pool *pool, int32_t slot, const void *x,
  */
 int32_t slora_set_option(slora_pool *pool, const char *key, int64_t value);
 
+/* ---------------------------------------------------------------------------------------------
+ * KV cache in 8 bits, in pages of the unified pool.
+ *
+ * A page holds a BLOCK of N = 8 * floor(page_H / (8 * head_dim)) tokens' K and V of ONE head of one
+ * layer, in granules of eight tokens: 8 * head_dim bytes of K, [token][element], then 8 * head_dim
+ * bytes of V, [element][token]; bytes beyond N tokens are not used.  A byte is a signed code c and
+ * stands for c * 2^e.  The exponent e belongs to the block: one for its K, one for its V.
+ *
+ *   e = the least integer >= -60 with |value| <= 127 * 2^e for every value the block has held,
+ *   c = value * 2^-e rounded to nearest, ties to even.
+ *
+ * A power of two makes every step exact but the rounding itself: a block whose exponent grows (a
+ * later token has larger values) has its codes shifted and rounded once more, and the same inputs
+ * give the same codes whatever computes them.  e = 127 marks a block that was given an infinity or
+ * a NaN: all of its K (or V) reads as NaN.
+ *
+ * Lengths are known to the host, page numbers live in a table on the device, and a batch is planned
+ * once for all layers.  For each step: extend, plan, then per layer append and attend; truncate
+ * when tokens are dropped.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct slora_kv8 slora_kv8;             /* a cache: page table, lengths */
+typedef struct slora_kv8_batch slora_kv8_batch; /* one batch's work lists and scratch */
+
+/*
+ * A cache for up to max_seqs sequences of up to max_tokens tokens in each of n_layers layers, on pages
+ * of `pool`.  n_heads query heads share n_kv_heads heads of K and V (n_heads % n_kv_heads == 0);
+ * head_dim is 32, 64, 96, 128, 192 or 256 and at most page_H / 8.  dev_exps: DEVICE memory of the caller
+ * (borrowed like the pool's), max_seqs * ceil(max_tokens / N) * n_layers * n_kv_heads * 2 bytes: the
+ * signed exponents [sequence][block][layer][head][K, V]; no particular content.  NULL for a host-only
+ * pool.  The library allocates the page table, 4 bytes for every two of those.
+ * slora_kv8_destroy waits for the device and releases the pages of all sequences; its batches must
+ * have been destroyed (EBUSY), and a pool is destroyed after its caches (EBUSY).
+ */
+int32_t slora_kv8_init(slora_kv8 **out, slora_pool *pool, int32_t n_layers, int32_t n_heads, int32_t n_kv_heads,
+                       int32_t head_dim, int32_t max_seqs, int32_t max_tokens, void *dev_exps);
+int32_t slora_kv8_destroy(slora_kv8 *cache);
+
+/*
+ * Fills out[0..n) (n <= SLORA_KV8_INFO_N) with [0] N, tokens of a block  [1] blocks of a sequence of max_tokens
+ * [2] pages a block takes over all layers and heads  [3] pages held.
+ */
+#define SLORA_KV8_INFO_N 4
+int32_t slora_kv8_info(const slora_kv8 *cache, int64_t *out, int32_t n);
+
+/* Tokens that the n sequences seqs[] (HOST) hold: out[i] (HOST). */
+int32_t slora_kv8_lengths(const slora_kv8 *cache, int32_t n, const int32_t *seqs, int32_t *out);
+
+/*
+ * Make room for tokens[i] >= 0 more tokens in sequence seqs[i] (HOST arrays, no sequence twice).  The pages
+ * of blocks that begin are page_idx[n_idx] (HOST), in the order [i][block][layer][head] - or, with
+ * page_idx == NULL and n_idx == 0, of the library's choice.  Host work only.
+ * Errors: ERANGE (sequence, length beyond max_tokens, page index), EINVAL (n_idx), EBUSY (page not free, listed
+ * twice; sequence twice), ENOMEM (fewer pages free than needed); nothing changes.
+ */
+int32_t slora_kv8_extend(slora_kv8 *cache, int32_t n, const int32_t *seqs, const int32_t *tokens,
+                         const int32_t *page_idx, int64_t n_idx);
+
+/*
+ * Cut sequence seqs[i] to lengths[i] tokens, at most what it holds, and free the pages of whole blocks
+ * behind them.  evicted == 0: the last tokens are dropped, as after drafted tokens that were refused
+ * (their positions are given out again).  evicted != 0: slora_kv8_evict has moved the tokens that stay to
+ * the front in every layer; positions go on from where they were.  Batches planned before with such a
+ * sequence become stale (EBUSY).  Launches in flight keep reading the freed pages: the caller orders
+ * their completion before other streams write them.
+ */
+int32_t slora_kv8_truncate(slora_kv8 *cache, int32_t n, const int32_t *seqs, const int32_t *lengths, int32_t evicted);
+
+/*
+ * Plan a batch of n sequences (HOST arrays, no sequence twice): rows[i] >= 0 query tokens of sequence
+ * seqs[i], in this order in q, k, v and out.  They are the last rows[i] tokens the sequence was extended
+ * by; row r of them sits in slot length - rows[i] + r.  keep: NULL, or for slora_kv8_evict how many tokens
+ * each sequence keeps (>= 0; a sequence that holds no more is left alone).
+ * The lists travel on the pool's upload stream; the first call of the batch waits for them on the device
+ * and brings new pages into the table.  All calls of a batch run in one order, as those of a slora_plan; the caller
+ * orders batches that share sequences (one stream, or events).  After its first call, a call whose
+ * kind was made before on that stream allocates nothing and may be captured in a HIP graph.
+ * slora_kv8_batch_destroy neither waits nor frees: buffers return to the pool.
+ */
+int32_t slora_kv8_batch_plan(slora_kv8 *cache, slora_kv8_batch **out, int32_t n, const int32_t *seqs, const int32_t *rows,
+                             const int32_t *keep);
+int32_t slora_kv8_batch_destroy(slora_kv8_batch *batch);
+
+/*
+ * Write K and V of the batch's tokens into the cache.  k, v: DEVICE, row t at k + t * k_stride, n_kv_heads * head_dim
+ * elements of the pool's storage type; strides in elements, multiples of 8; 16-byte aligned.
+ * Refused (EINVAL) if a sequence has fewer tokens than rows.
+ */
+int32_t slora_kv8_append(slora_kv8_batch *batch, int32_t layer, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, void *stream);
+
+/*
+ * out[t, h] = sum_j p_j V_j,  p = softmax_j(scale * q[t, h] . K_j), over the tokens j the cache holds for t's
+ * sequence; with causal != 0 those up to t's own slot.  q, out: DEVICE, row t at q + t * q_stride, [n_heads][head_dim] of
+ * the pool's storage type, aligned as above; head h reads head h / (n_heads / n_kv_heads) of the cache.  A row that
+ * sees no token is 0.  Products and sums are fp32; p is rounded to 11 bits for the second product.
+ * weights_in, weights_out, pos: NULL, or DEVICE arrays [max_seqs][n_kv_heads][max_tokens] of this layer:
+ *   weights_out[j] = weights_in[j] (0 for the batch's own tokens) + sum of p_j over the sequence's rows and the heads that share j's head,
+ *   in fp32; pos[j] = position of j, written for the batch's own tokens.
+ * weights_in may be weights_out.  Only entries of the sequences' tokens are touched.  Results do not depend on
+ * what else runs: no floating-point atomics, one order per batch.
+ */
+int32_t slora_kv8_attend(slora_kv8_batch *batch, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                         float scale, int32_t causal, const float *weights_in, float *weights_out, int32_t *pos, void *stream);
+
+/*
+ * Of each head's tokens keep[i] stay (see the plan): those whose position is among the last
+ * min(recent, keep[i]) ones given out, then those of greatest weight, of equal weights those in lower slots (a NaN counts as greater than any
+ * number).  In order of slots, the tokens that stay behind slot keep[i] move into the places before it that fall free; the others do
+ * not move.  A block that takes tokens of a larger exponent is shifted to it.  weights_out and pos_out
+ * get the entries of slots before keep[i]; they may be weights_in and pos_in.  When all layers have been
+ * done, slora_kv8_truncate(..., evicted = 1) frees the pages behind.
+ */
+int32_t slora_kv8_evict(slora_kv8_batch *batch, int32_t layer, int32_t recent, const float *weights_in, float *weights_out,
+                        const int32_t *pos_in, int32_t *pos_out, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Products with 4-bit weights: y[t, o] = sum_k x[t, k] * (c[o, k] - z[o, g]) * s[o, g],  g = k / group - the base
+ * model's xW (Fig. 1) of a decode batch, onto which slora_lora_apply adds.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct slora_w4 slora_w4;
+
+/*
+ * Lay out one matrix for the product.  codes: DEVICE [outputs][inputs / 2] bytes, input k in the low (even k) or high four bits;
+ * scales: DEVICE [outputs][ceil(inputs / group)] elements of `dtype`; zeros: DEVICE bytes 0 .. 15 of the same shape,
+ * or NULL for 8 throughout.  inputs % 8 == 0; group % 32 == 0.  packed: DEVICE, slora_w4_bytes(...) bytes, 16-byte
+ * aligned, borrowed until slora_w4_destroy; it is written by a kernel on `stream`, after which codes, scales
+ * and zeros are no longer needed.  The matrix belongs to the HIP device that is current.
+ */
+int32_t slora_w4_bytes(int32_t outputs, int32_t inputs, int32_t group, int64_t *out);
+int32_t slora_w4_pack(slora_w4 **out, int32_t outputs, int32_t inputs, int32_t group, int32_t dtype, const void *codes,
+                      const void *scales, const uint8_t *zeros, void *packed, void *stream);
+int32_t slora_w4_destroy(slora_w4 *w);
+
+/*
+ * The product for n <= SLORA_MAX_MULTI matrices in one launch.  x[k]: DEVICE, T rows of w[k]'s inputs, in its 16-bit
+ * type, 16-byte aligned (entries may be equal); y[k]: DEVICE, T rows of its outputs, fp32 or (_y16) its 16-bit type, written, not
+ * added to; 16-byte aligned.  All matrices have one type and one group size.  Sums are fp32, in an order that
+ * depends on the shapes alone.  A token with an infinite or NaN x has NaN (or infinite) outputs, other tokens are
+ * not affected.  Allocates nothing; may be captured in a HIP graph.
+ */
+int32_t slora_w4_matmul(int32_t n, const slora_w4 *const *w, const void *const *x, int32_t T, float *const *y, void *stream);
+int32_t slora_w4_matmul_y16(int32_t n, const slora_w4 *const *w, const void *const *x, int32_t T, void *const *y, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

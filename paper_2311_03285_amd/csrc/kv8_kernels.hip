@@ -1,0 +1,836 @@
+// gfx950 kernels of the 8-bit KV cache: append, attention, the weights that cached tokens draw, eviction.
+//
+// Layout (see slora.h): a page holds a block of N tokens of one head, in granules of eight - 8 * D bytes of
+// K as [token][element], 8 * D bytes of V as [element][token].  A code c stands for c * 2^e, e by block.
+// All byte offsets into the pool are 64-bit.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "kv8.hpp"
+
+namespace slora {
+
+namespace {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWave = 64;
+
+template <int DT>
+__device__ __forceinline__ float widen(uint16_t b)
+{
+    return DT == SLORA_F16 ? (float)__builtin_bit_cast(_Float16, b) : __uint_as_float((uint32_t)b << 16);
+}
+template <int DT>
+__device__ __forceinline__ uint16_t narrow(float f)
+{
+    if constexpr (DT == SLORA_F16)
+        return __builtin_bit_cast(uint16_t, (_Float16)f);
+    else
+        return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+
+__device__ __forceinline__ float across_16(float v) { return __shfl_xor(v, 16, kWave); }
+__device__ __forceinline__ float across_32(float v) { return __shfl_xor(v, 32, kWave); }
+
+// n / (granules per block) for n < 2^17 or so many: div = ceil(2^32 / d) is exact while n * d < 2^32; 0 stands for d = 1
+__device__ __forceinline__ uint32_t kv_div(uint32_t n, uint32_t div) { return div ? __umulhi(n, div) : n; }
+
+__device__ __forceinline__ int64_t table_entry(const KvShape &s, int seq, int block, int head)
+{
+    return (((int64_t)seq * s.max_blocks + block) * s.n_layers + s.layer) * s.n_kv + head;
+}
+
+// 2^e of a block: NaN for one that holds an infinity or NaN
+__device__ __forceinline__ float unit_of(int e) { return e == kKvPoison ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// least e >= kKvLowest with amax <= 127 * 2^e = 1.984375 * 2^(e + 6); amax >= 0
+__device__ __forceinline__ int exponent_of(float amax)
+{
+    const int32_t bits = __float_as_int(amax);
+    if (bits >= 0x7f800000) return kKvPoison;
+    return max(((bits - 0x7e0001) >> 23) - 132, kKvLowest);
+}
+
+// code of `v` in units of 2^e (|v| <= 127 * 2^e): the product is exact, so this is the only rounding
+__device__ __forceinline__ int code_of(float v, float inverse) { return (int)__builtin_rintf(v * inverse); }
+
+// 2^-e of a block without infinities (e <= 122: the bits of a normal number)
+__device__ __forceinline__ float inverse_of(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
+
+// the four codes in `u` in units 2^shift times larger (shift >= 0): each rounded to nearest, ties to even
+__device__ __forceinline__ uint32_t shift_codes(uint32_t u, float factor)
+{
+    uint32_t r = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r |= ((uint32_t)(int)__builtin_rintf((float)(int8_t)(u >> (8 * k)) * factor) & 0xffu) << (8 * k);
+    return r;
+}
+__device__ __forceinline__ float shift_factor(int from, int to) // both exponents of a block; 0 where it becomes poisoned
+{
+    return to == kKvPoison || to - from > 100 ? 0.0f : __uint_as_float((uint32_t)(127 - (to - from)) << 23);
+}
+
+// ---------------------------------------------------------------------------------------
+// page table
+// ---------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void kv_table_kernel(int32_t *__restrict__ table, const int32_t *__restrict__ columns, const int32_t *__restrict__ pages, int per)
+{
+    const int64_t to = (int64_t)columns[blockIdx.x] * per, from = (int64_t)blockIdx.x * per;
+    for (int i = threadIdx.x; i < per; i += blockDim.x) table[to + i] = pages[from + i];
+}
+
+// ---------------------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------------------
+// A workgroup = the new tokens of one block and head; wavefront 0 writes K, wavefront 1 V.  Each reads its rows twice (the second time
+// they are in the caches): once for the largest value, once to round them.  K: 16 bytes of a row a lane.  V, which is
+// stored transposed: a lane has two elements of the eight tokens of a granule, reads them as 4 bytes of eight rows and writes
+// 16 bytes; what the granule held before stays, in new units if the exponent has grown.
+template <int DT>
+__global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAppend a)
+{
+    const KvItem it = items[blockIdx.x / s.n_kv];
+    const int head = blockIdx.x % s.n_kv, which = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t entry = table_entry(s, seqs[it.s].seq, it.a, head);
+    uint8_t *page = s.pool + (int64_t)s.table[entry] * s.page_bytes;
+    const int D = s.D, t0 = it.b, n = it.c;
+    const uint16_t *x = a.x[which] + (int64_t)it.d * a.stride[which] + (int64_t)head * D;
+    const int64_t stride = a.stride[which];
+    const int before = t0 > 0 ? s.exps[2 * entry + which] : kKvLowest;
+
+    // 16 bytes a lane: D / 8 lanes to a row
+    const int per_row = D / 8, rows_at_once = kWave / per_row, r0 = lane / per_row, c0 = lane % per_row * 8;
+    const bool on = r0 < rows_at_once;
+    uint32_t top = 0; // largest magnitude, as the bits of its 16-bit form (which order as the values do)
+    for (int r = r0; on && r < n; r += rows_at_once) {
+        const u32x4 u = *reinterpret_cast<const u32x4 *>(x + r * stride + c0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = max(top, max(u[k] & 0x7fffu, (u[k] >> 16) & 0x7fffu));
+    }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, kWave));
+    const int e = max(before, exponent_of(widen<DT>((uint16_t)top)));
+    const bool poison = e == kKvPoison;
+    const float inverse = poison ? 0.0f : inverse_of(e);
+    const bool grown = e != before;
+    const float factor = shift_factor(before, e);
+
+    if (which == 0) {
+        // slot t of the block: granule t / 8, row t % 8
+        auto row_at = [&](int t) { return page + (int64_t)(t / kKvGranule) * (2 * kKvGranule * D) + (t % kKvGranule) * D; };
+        if (grown)
+            for (int t = r0; on && t < t0; t += rows_at_once) {
+                u32x2 *p = reinterpret_cast<u32x2 *>(row_at(t) + c0);
+                u32x2 u = *p;
+                u.x = shift_codes(u.x, factor);
+                u.y = shift_codes(u.y, factor);
+                *p = u;
+            }
+        for (int r = r0; on && r < n; r += rows_at_once) {
+            const u32x4 u = *reinterpret_cast<const u32x4 *>(x + r * stride + c0);
+            uint32_t o[2] = {0, 0};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float v = widen<DT>((uint16_t)(u[k / 2] >> (16 * (k % 2))));
+                if (!poison) o[k / 4] |= ((uint32_t)code_of(v, inverse) & 0xffu) << (8 * (k % 4));
+            }
+            *reinterpret_cast<u32x2 *>(row_at(t0 + r) + c0) = u32x2{o[0], o[1]};
+        }
+    } else {
+        const int first = grown ? 0 : t0 / kKvGranule, last = (t0 + n - 1) / kKvGranule;
+        const int pairs = D / 2;
+        for (int w = lane; w < pairs * (last - first + 1); w += kWave) {
+            const int g = first + w / pairs, d = w % pairs * 2;
+            u32x4 *p = reinterpret_cast<u32x4 *>(page + (int64_t)g * (2 * kKvGranule * D) + kKvGranule * D + d * kKvGranule);
+            const int lo = g * kKvGranule, from = max(t0 - lo, 0), to = min(t0 + n - lo, kKvGranule); // its new tokens: [from, to)
+            uint32_t u[4] = {0, 0, 0, 0}; // element d: slots 0 .. 3, 4 .. 7; element d + 1
+            if (from > 0 || to < kKvGranule) {
+                const u32x4 all = *p;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    u[k] = all[k];
+                    const int mine = min(max(from - 4 * (k % 2), 0), 4); // slots before t0; those behind the new ones are nobody's
+                    const uint32_t mask = mine == 4 ? 0xffffffffu : (1u << (8 * mine)) - 1;
+                    if (grown) u[k] = (shift_codes(u[k], factor) & mask) | (u[k] & ~mask);
+                }
+            }
+            uint32_t raw[kKvGranule];
+#pragma unroll
+            for (int t = 0; t < kKvGranule; ++t) raw[t] = t >= from && t < to ? *reinterpret_cast<const uint32_t *>(x + (lo + t - t0) * stride + d) : 0;
+#pragma unroll
+            for (int t = 0; t < kKvGranule; ++t) {
+                if (t < from || t >= to) continue;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float v = widen<DT>((uint16_t)(raw[t] >> (16 * h)));
+                    const uint32_t c = poison ? 0u : (uint32_t)code_of(v, inverse) & 0xffu;
+                    uint32_t &word = u[2 * h + t / 4];
+                    word = (word & ~(0xffu << (8 * (t % 4)))) | (c << (8 * (t % 4)));
+                }
+            }
+            *p = u32x4{u[0], u[1], u[2], u[3]};
+        }
+    }
+    if (lane == 0) s.exps[2 * entry + which] = (int8_t)e;
+}
+
+// ---------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------
+// Matrix instruction 16 x 16 x 32 (f16): lane l = 16 g + n supplies k-values 8 g .. 8 g + 7 of row (first operand) or column
+// (second) n, and receives rows 4 g .. 4 g + 3 of column n.
+//
+// A wavefront takes 32 tokens (four granules) and 16 columns (a column = a query row and one of the heads that share the
+// cache's head) at a time, with the scores transposed: S' = K Q', so that a lane's scores are of ONE column.  Rows of S' may
+// be any tokens: row 4 g + i of its half t is token 4 t + i of granule g, so that lane (g, n) ends with the scores of all eight tokens of
+// granule g - the k-values it has to supply for O' = V' P', whose first operand is eight bytes of V: probabilities go
+// from one product to the next in the registers where they are, and K and V come from memory straight
+// into operands.  Codes become binary16 exactly (|c| <= 127); q in bfloat16 is scaled by a power of two of its own into the range of
+// binary16, which keeps its eight bits down to 2^-28 of the row's largest.
+//
+// Softmax: with scores s (times log2 e) and V's exponents ev, the running maximum is of s + ev, so that
+// p = 2^(s + ev - m) <= 1 is what the second product needs of V's units, as a binary16 number; the sum that divides takes p * 2^-ev.
+__device__ __forceinline__ f32x4 mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// four codes -> binary16: 0x6400 | u is 1024 + u for a byte u; c + 128 = u
+__device__ __forceinline__ void codes_to_f16(uint32_t u, half2_t &a, half2_t &b)
+{
+    u ^= 0x80808080u;
+    const half2_t bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias;
+    b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias;
+}
+__device__ __forceinline__ f16x8 codes_to_f16x8(uint32_t lo, uint32_t hi)
+{
+    half2_t r[4];
+    codes_to_f16(lo, r[0], r[1]);
+    codes_to_f16(hi, r[2], r[3]);
+    return __builtin_shufflevector(__builtin_shufflevector(r[0], r[1], 0, 1, 2, 3), __builtin_shufflevector(r[2], r[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Which element of a head the operands of step j hold in k-value i of lane group g: K's rows are read 16 bytes a lane, two
+// steps at a time; the last step of an odd number reads 8.
+template <int DB>
+__device__ __forceinline__ int element_of(int j, int g)
+{
+    return j / 2 * 2 + 1 < DB ? j / 2 * 64 + 16 * g + 8 * (j % 2) : j * 32 + 8 * g;
+}
+
+// q of one column as second operands, and the power of two to multiply its scores by
+template <int DT, int DB>
+__device__ __forceinline__ void load_q(const uint16_t *q, int g, f16x8 (&f)[DB], float &unit)
+{
+    unit = 1.0f;
+    if constexpr (DT == SLORA_F16) {
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+            f[j] = q ? __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(q + element_of<DB>(j, g))) : f16x8{};
+    } else {
+        u32x4 raw[DB];
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < DB; ++j) {
+            raw[j] = q ? *reinterpret_cast<const u32x4 *>(q + element_of<DB>(j, g)) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, max(raw[j][k] & 0x7fffu, (raw[j][k] >> 16) & 0x7fffu));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, kWave));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
+        // largest magnitude 2^(x - 127) .. : times 2^(141 - x) it lies in [2^14, 2^15); both powers are kept normal numbers
+        const int x = (int)(top >> 7);
+        const int up = x == 0 || x == 255 ? 0 : min(max(141 - x, -100), 100);
+        const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+        unit = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[j][k] = (_Float16)(__uint_as_float((raw[j][k / 2] >> (16 * (k % 2))) << 16) * scale);
+    }
+}
+
+// K of one token as first operands, from its row
+template <int DB>
+__device__ __forceinline__ void load_k(const uint8_t *row, int g, u32x4 (&raw)[(DB + 1) / 2])
+{
+#pragma unroll
+    for (int p = 0; p < (DB + 1) / 2; ++p) {
+        if (2 * p + 1 < DB) {
+            raw[p] = *reinterpret_cast<const u32x4 *>(row + 64 * p + 16 * g);
+        } else {
+            const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 64 * p + 8 * g);
+            raw[p] = u32x4{u.x, u.y, 0u, 0u};
+        }
+    }
+}
+template <int DB>
+__device__ __forceinline__ f16x8 k_operand(const u32x4 (&raw)[(DB + 1) / 2], int j)
+{
+    return j % 2 ? codes_to_f16x8(raw[j / 2].z, raw[j / 2].w) : codes_to_f16x8(raw[j / 2].x, raw[j / 2].y);
+}
+
+// Pages and exponents of the blocks of a part, in LDS
+struct PartPages {
+    int32_t page[kKvPartBlocks];
+    int16_t e[kKvPartBlocks]; // K in the low byte, V above
+};
+__device__ __forceinline__ void load_pages(PartPages &pp, const KvShape &s, int seq, int head, int block0, int blocks)
+{
+    for (int i = threadIdx.x; i < blocks; i += blockDim.x) {
+        const int64_t entry = table_entry(s, seq, block0 + i, head);
+        pp.page[i] = s.table[entry];
+        pp.e[i] = reinterpret_cast<const int16_t *>(s.exps)[entry];
+    }
+}
+
+// A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
+// maxima, sums and O', and are put together in LDS at the end.
+template <int DT, int DB>
+__global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
+{
+    constexpr int D = DB * 32, kWaves = kKvFewThreads / kWave;
+    __shared__ PartPages pp;
+    __shared__ float merge_ml[kWaves][kKvFewCols][2];
+    __shared__ float merge_o[kWaves][kKvFewCols][D];
+    const KvItem it = items[blockIdx.x / s.n_kv];
+    const int head = blockIdx.x % s.n_kv;
+    const KvSeq q = seqs[it.s];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
+    const int gpb = s.N / kKvGranule;
+
+    // this lane's column, and how many tokens it sees
+    const int col = it.a + n, row = col / s.G;
+    const bool real = n < it.b;
+    const int old = q.len - q.rows;
+    const int limit = !real ? 0 : a.causal ? min(old + row + 1, q.len) : q.len;
+    const int last_row = (it.a + it.b - 1) / s.G;
+    const int tokens = a.causal ? min(old + last_row + 1, q.len) : q.len;
+    const int g1 = min(it.d, (max(tokens, 0) + kKvGranule - 1) / kKvGranule), g0 = it.c;
+    const int block0 = g0 / gpb, base = block0 * gpb;
+    if (g1 > g0) load_pages(pp, s, q.seq, head, block0, (g1 - 1) / gpb + 1 - block0);
+
+    f16x8 qf[DB];
+    float unit;
+    const int qhead = head * s.G + col % s.G;
+    load_q<DT, DB>(real ? a.q + (int64_t)(q.row0 + row) * a.q_stride + (int64_t)qhead * D : nullptr, g, qf, unit);
+    unit *= a.scale;
+    __syncthreads();
+
+    f32x4 o[2 * DB];
+#pragma unroll
+    for (int k = 0; k < 2 * DB; ++k) o[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -INFINITY, l = 0.0f;
+
+    // of the granules of a chunk, a lane reads K rows of number n / 4 (4 t + n % 4 of it) and V of number g, whose scores it gets
+    u32x4 kr[2][(DB + 1) / 2], vr[DB];
+    int e_next = 0;
+    auto fetch = [&](int gr) {
+        const int gk = min(gr + n / 4, g1 - 1) - base, gv = min(gr + g, g1 - 1) - base;
+        const int bk = (int)kv_div((uint32_t)gk, s.div_b), bv = (int)kv_div((uint32_t)gv, s.div_b);
+        const uint8_t *pk = s.pool + (int64_t)pp.page[bk] * s.page_bytes + (int64_t)(gk - bk * gpb) * (2 * kKvGranule * D) + (n % 4) * D;
+        const uint8_t *pv = s.pool + (int64_t)pp.page[bv] * s.page_bytes + (int64_t)(gv - bv * gpb) * (2 * kKvGranule * D) + kKvGranule * D + n * 16;
+        load_k<DB>(pk, g, kr[0]);
+        load_k<DB>(pk + 4 * D, g, kr[1]);
+#pragma unroll
+        for (int k = 0; k < DB; ++k) vr[k] = *reinterpret_cast<const u32x4 *>(pv + k * 256);
+        e_next = pp.e[bv];
+    };
+    int gr = g0 + wave * (kKvChunk / kKvGranule);
+    if (gr < g1) fetch(gr);
+    for (; gr < g1;) {
+        // operands of this chunk, then the next chunk's loads
+        f32x4 sc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            sc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < DB; ++j) sc[t] = mfma16(k_operand<DB>(kr[t], j), qf[j], sc[t]);
+        }
+        u32x4 v[DB];
+#pragma unroll
+        for (int k = 0; k < DB; ++k) v[k] = vr[k];
+        const int ek = (int8_t)(e_next & 0xff), ev = e_next >> 8;
+        const int token = (gr + g) * kKvGranule;
+        const int bound = min(limit, g1 * kKvGranule) - token; // tokens of this lane's granule that its column sees
+        gr += kWaves * (kKvChunk / kKvGranule);
+        if (gr < g1) fetch(gr);
+
+        const float f = unit * unit_of(ek), add = ev == kKvPoison ? __uint_as_float(0x7fc00000u) : (float)ev;
+        float t[8], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t[i] = i < bound ? __builtin_fmaf(sc[i / 4][i % 4], f, add) : -INFINITY;
+            top = fmaxf(top, t[i]);
+        }
+        top = fmaxf(top, across_16(top));
+        top = fmaxf(top, across_32(top));
+        const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float keep = __builtin_amdgcn_exp2f(m - m_use);
+        m = m_new;
+        float sum = 0.0f;
+        f16x8 p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = __builtin_amdgcn_exp2f(t[i] - m_use);
+            sum += x;
+            p[i] = (_Float16)x;
+        }
+        l = __builtin_fmaf(l, keep, bound > 0 ? sum * unit_of(-ev) : 0.0f);
+        if (__any(keep != 1.0f)) {
+#pragma unroll
+            for (int k = 0; k < 2 * DB; ++k) o[k] *= keep;
+        }
+        // element 32 k + 2 m + h of row m of o[2 k + h]
+#pragma unroll
+        for (int k = 0; k < DB; ++k) {
+            o[2 * k] = mfma16(codes_to_f16x8(v[k].x, v[k].y), p, o[2 * k]);
+            o[2 * k + 1] = mfma16(codes_to_f16x8(v[k].z, v[k].w), p, o[2 * k + 1]);
+        }
+    }
+    l += across_16(l);
+    l += across_32(l);
+
+    if (real) {
+        if (g == 0) {
+            merge_ml[wave][n][0] = m;
+            merge_ml[wave][n][1] = l;
+        }
+#pragma unroll
+        for (int k = 0; k < DB; ++k) // elements 32 k + 8 g .. + 7
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                merge_o[wave][n][32 * k + 8 * g + 2 * i] = o[2 * k][i];
+                merge_o[wave][n][32 * k + 8 * g + 2 * i + 1] = o[2 * k + 1][i];
+            }
+    }
+    __syncthreads();
+    for (int w = (int)threadIdx.x; w < it.b * (D / 8); w += kKvFewThreads) {
+        const int c = w / (D / 8), d = w % (D / 8) * 8;
+        float top = -INFINITY, total = 0.0f, sum[8] = {};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, merge_ml[k][c][0]);
+        const float use = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float x = __builtin_amdgcn_exp2f(merge_ml[k][c][0] - use);
+            total = __builtin_fmaf(merge_ml[k][c][1], x, total);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(merge_o[k][c][d + i], x, sum[i]);
+        }
+        if (it.poff >= 0) {
+            const int64_t at = (int64_t)(it.poff + c) * s.n_kv + head;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a.part_o[at * D + d + i] = sum[i];
+            if (d == 0) {
+                a.part_ml[2 * at] = top;
+                a.part_ml[2 * at + 1] = total;
+            }
+        } else {
+            const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
+            const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
+            u32x4 u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = (uint32_t)narrow<DT>(sum[2 * i] * by) | ((uint32_t)narrow<DT>(sum[2 * i + 1] * by) << 16);
+            *reinterpret_cast<u32x4 *>(a.out + (int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + d) = u;
+            if (d == 0) {
+                float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
+                st[0] = use;
+                st[1] = by;
+            }
+        }
+    }
+}
+
+// Parts of a column put together, in the order of the sequence.  A workgroup = the columns of one tile, a wavefront one at a time.
+template <int DT, int DB>
+__global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
+{
+    constexpr int D = DB * 32, kPer = (D + kWave - 1) / kWave; // elements of a lane
+    const KvItem it = items[blockIdx.x / s.n_kv];
+    const int head = blockIdx.x % s.n_kv;
+    const KvSeq q = seqs[it.s];
+    const int lane = threadIdx.x % kWave;
+    for (int c = threadIdx.x / kWave; c < it.b; c += 256 / kWave) {
+        float top = -INFINITY;
+        for (int k = lane; k < it.c; k += kWave) top = fmaxf(top, a.part_ml[2 * ((int64_t)(it.poff + (int64_t)k * it.b + c) * s.n_kv + head)]);
+#pragma unroll
+        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
+        const float use = top == -INFINITY ? 0.0f : top;
+        float total = 0.0f, sum[kPer] = {};
+        for (int k = 0; k < it.c; ++k) {
+            const int64_t at = (int64_t)(it.poff + (int64_t)k * it.b + c) * s.n_kv + head;
+            const float x = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use);
+            total = __builtin_fmaf(a.part_ml[2 * at + 1], x, total);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (lane + 64 * i < D) sum[i] = __builtin_fmaf(a.part_o[at * D + lane + 64 * i], x, sum[i]);
+        }
+        const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
+        const float by = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (lane + 64 * i < D) a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + lane + 64 * i] = narrow<DT>(sum[i] * by);
+        if (lane == 0) {
+            float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
+            st[0] = use;
+            st[1] = by;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// what cached tokens draw
+// ---------------------------------------------------------------------------------------
+// The scores once more, 32 tokens a wavefront, with the maxima and sums that attention left; a lane adds up its tokens over its column of
+// every tile, then the 16 columns are added.
+template <int DT, int DB>
+__global__ __launch_bounds__(kKvFewThreads) void kv_weights_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvAttend a, KvWeights out)
+{
+    constexpr int D = DB * 32, kWaves = kKvFewThreads / kWave;
+    const KvSeq q = seqs[blockIdx.z];
+    const int head = blockIdx.y;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
+    const int gr = (blockIdx.x * kWaves + wave) * (kKvChunk / kKvGranule), granules = (q.len + kKvGranule - 1) / kKvGranule;
+    if (gr >= granules) return;
+    const int gpb = s.N / kKvGranule, old = q.len - q.rows;
+    u32x4 kr[2][(DB + 1) / 2];
+    const int gk = min(gr + n / 4, granules - 1), gv = min(gr + g, granules - 1);
+    const uint8_t *pk = s.pool + (int64_t)s.table[table_entry(s, q.seq, gk / gpb, head)] * s.page_bytes + (int64_t)(gk % gpb) * (2 * kKvGranule * D) + (n % 4) * D;
+    load_k<DB>(pk, g, kr[0]);
+    load_k<DB>(pk + 4 * D, g, kr[1]);
+    const int ek = s.exps[2 * table_entry(s, q.seq, gv / gpb, head)];
+    f16x8 kf[2][DB];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < DB; ++j) kf[t][j] = k_operand<DB>(kr[t], j);
+    const int token = (gr + g) * kKvGranule, cols = q.rows * s.G;
+    float w[8] = {};
+    // rows before the chunk's first token see none of it
+    for (int c0 = a.causal ? max(gr * kKvGranule - old, 0) * s.G / 16 * 16 : 0; c0 < cols; c0 += 16) {
+        const int col = c0 + n, row = col / s.G, h = head * s.G + col % s.G;
+        const bool real = col < cols;
+        f16x8 qf[DB];
+        float unit;
+        load_q<DT, DB>(real ? a.q + (int64_t)(q.row0 + row) * a.q_stride + (int64_t)h * D : nullptr, g, qf, unit);
+        const float *st = a.stat + 2 * ((int64_t)(q.row0 + row) * s.n_kv * s.G + h);
+        const float m = real ? st[0] : 0.0f, by = real ? st[1] : 0.0f;
+        const float f = unit * a.scale * unit_of(ek);
+        const int bound = (!real ? 0 : a.causal ? min(old + row + 1, q.len) : q.len) - token;
+        f32x4 sc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            sc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < DB; ++j) sc[t] = mfma16(kf[t][j], qf[j], sc[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < bound) w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 4][i % 4], f, -m)), by, w[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int x = 8; x; x >>= 1) w[i] += __shfl_xor(w[i], x, kWave);
+    if (n < 8 && token + n < q.len) {
+        float v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v = n == i ? w[i] : v;
+        const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens + token + n;
+        if (token + n < old)
+            v += out.w_in[at];
+        else
+            out.pos[at] = q.seen - q.rows + token + n - old;
+        out.w_out[at] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// eviction
+// ---------------------------------------------------------------------------------------
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+
+// numbers in the order of the weights: recent tokens above everything, then NaN, then values; -0 is 0
+__device__ __forceinline__ uint32_t rank_of(float w, int32_t pos, int32_t recent_from)
+{
+    if (pos >= recent_from) return 0xffffffffu;
+    if (w != w) return 0xfffffffeu;
+    const uint32_t u = __float_as_uint(w + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// One workgroup per sequence and head.  The rank of the last token that stays is found eight bits at a time; then every wavefront takes
+// a run of slots, and counts say where its places and moves go in the lists: all integers, in the order of the slots.
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
+{
+    __shared__ uint32_t bins[256];
+    __shared__ uint32_t found[2];
+    __shared__ int counts[3][kEvictWaves];
+    const KvSeq q = seqs[blockIdx.x / s.n_kv];
+    const int head = blockIdx.x % s.n_kv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens;
+    const float *w = e.w_in + at;
+    const int32_t *pos = e.pos_in + at;
+    if (q.keep >= q.len) {
+        for (int i = threadIdx.x; i < q.len; i += kEvictThreads) {
+            e.w_out[at + i] = w[i];
+            e.pos_out[at + i] = pos[i];
+        }
+        return;
+    }
+    if (q.keep == 0) return;
+    const int recent_from = q.seen - min(min(e.recent, q.keep), q.seen);
+    // the rank of the keep-th token, and how many of that rank stay
+    uint32_t prefix = 0;
+    int left = q.keep;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (threadIdx.x < 256) bins[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < q.len; i += kEvictThreads) {
+            const uint32_t r = rank_of(w[i], pos[i], recent_from);
+            if (shift == 24 || (r >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[(r >> shift) & 255u], 1u);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            int k = 255;
+            uint32_t above = 0;
+            while (k > 0 && above + bins[k] < (uint32_t)left) above += bins[k--];
+            found[0] = (uint32_t)k;
+            found[1] = above;
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        left -= (int)found[1];
+        __syncthreads();
+    }
+    // slots of this wavefront
+    const int run = ((q.len + kEvictWaves - 1) / kEvictWaves + kWave - 1) / kWave * kWave;
+    const int lo = wave * run, hi = min(lo + run, q.len);
+    auto before = [&](const int (&c)[kEvictWaves]) {
+        int b = 0;
+        for (int k = 0; k < wave; ++k) b += c[k];
+        return b;
+    };
+    int equal = 0;
+    for (int i = lo + lane; i - lane < hi; i += kWave) equal += __popcll(__ballot(i < hi && rank_of(w[i], pos[i], recent_from) == prefix));
+    if (lane == 0) counts[0][wave] = equal;
+    __syncthreads();
+    const int equal_before = before(counts[0]);
+    const uint64_t lower = (uint64_t(1) << lane) - 1;
+    // calls f(slot, stays) for 64 slots at a time
+    auto walk = [&](auto f) {
+        int seen = equal_before;
+        for (int i = lo + lane; i - lane < hi; i += kWave) {
+            const uint32_t r = i < hi ? rank_of(w[i], pos[i], recent_from) : 0;
+            const uint64_t same = __ballot(i < hi && r == prefix);
+            f(i, i < hi && (r > prefix || (r == prefix && seen + (int)__popcll(same & lower) < left)));
+            seen += __popcll(same);
+        }
+    };
+    int holes = 0, moves = 0;
+    walk([&](int i, bool stays) {
+        holes += __popcll(__ballot(i < hi && i < q.keep && !stays));
+        moves += __popcll(__ballot(i < hi && i >= q.keep && stays));
+    });
+    if (lane == 0) {
+        counts[1][wave] = holes;
+        counts[2][wave] = moves;
+    }
+    __syncthreads();
+    holes = before(counts[1]);
+    moves = before(counts[2]);
+    int total = 0;
+    for (int k = 0; k < kEvictWaves; ++k) total += counts[2][k];
+    const int most = min(q.keep, q.len - q.keep), blocks = (q.keep + s.N - 1) / s.N;
+    int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
+    int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
+    walk([&](int i, bool stays) {
+        const bool hole = i < hi && i < q.keep && !stays, move = i < hi && i >= q.keep && stays;
+        const uint64_t hs = __ballot(hole), ms = __ballot(move);
+        const int h = holes + __popcll(hs & lower);
+        if (i < hi && i < q.keep && i % s.N == 0) first[i / s.N] = h;
+        if (hole) dst[h] = i;
+        if (move) {
+            const int m = moves + __popcll(ms & lower);
+            src[m] = i;
+            const int16_t both = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, i / s.N, head)];
+            ex[m] = (int32_t)(int8_t)(both & 0xff) & 0xffff;
+            ex[m] |= (int32_t)(both >> 8) << 16;
+        }
+        holes += __popcll(hs);
+        moves += __popcll(ms);
+    });
+    if (threadIdx.x == 0) first[blocks] = total;
+    __syncthreads();
+    // (entries of slots from keep on are only read)
+    for (int i = threadIdx.x; i < total; i += kEvictThreads) {
+        e.w_out[at + dst[i]] = w[src[i]];
+        e.pos_out[at + dst[i]] = pos[src[i]];
+    }
+    if (e.w_out != e.w_in || e.pos_out != e.pos_in) {
+        // the places that are not in the list, between those that are
+        for (int k = threadIdx.x / kWave; k <= total; k += kEvictWaves) {
+            const int from = k ? dst[k - 1] + 1 : 0, to = k < total ? dst[k] : q.keep;
+            for (int i = from + lane; i < to; i += kWave) {
+                if (e.w_out != e.w_in) e.w_out[at + i] = w[i];
+                if (e.pos_out != e.pos_in) e.pos_out[at + i] = pos[i];
+            }
+        }
+    }
+}
+
+// One workgroup per block that keeps tokens, and head.  Nobody writes slots from keep on, and nobody else this block's.
+__global__ __launch_bounds__(128) void kv_evict_move_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
+{
+    const KvSeq q = seqs[blockIdx.z];
+    const int head = blockIdx.y, block = blockIdx.x, D = s.D;
+    const int blocks = (q.keep + s.N - 1) / s.N;
+    if (q.keep >= q.len || block >= blocks) return;
+    const int most = min(q.keep, q.len - q.keep);
+    const int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
+    const int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
+    const int m0 = first[block], m1 = first[block + 1];
+    if (m0 == m1) return;
+    const int64_t entry = table_entry(s, q.seq, block, head);
+    uint8_t *page = s.pool + (int64_t)s.table[entry] * s.page_bytes;
+    const int was[2] = {s.exps[2 * entry], s.exps[2 * entry + 1]};
+    int now[2] = {was[0], was[1]};
+    for (int m = m0; m < m1; ++m) {
+        now[0] = max(now[0], (int)(int16_t)(ex[m] & 0xffff));
+        now[1] = max(now[1], ex[m] >> 16);
+    }
+    __syncthreads(); // every thread has read the exponents
+    const int last = min(s.N, q.keep - block * s.N); // slots of the block that stay in use
+    const int words = D / 4;
+    if (now[0] != was[0]) {
+        const float f = shift_factor(was[0], now[0]);
+        for (int w = threadIdx.x; w < last * words; w += 128) {
+            const int t = w / words;
+            uint32_t *p = reinterpret_cast<uint32_t *>(page + (int64_t)(t / kKvGranule) * (2 * kKvGranule * D) + (t % kKvGranule) * D) + w % words;
+            *p = shift_codes(*p, f);
+        }
+    }
+    if (now[1] != was[1]) {
+        const float f = shift_factor(was[1], now[1]);
+        // four slots of an element at a time; a granule that others still read has slots behind `last`
+        for (int w = threadIdx.x; w < (last + 3) / 4 * D; w += 128) {
+            const int quad = w / D, d = w % D, t = quad * 4;
+            uint8_t *p = page + (int64_t)(t / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + d * kKvGranule + t % kKvGranule;
+            const uint32_t u = shift_codes(*reinterpret_cast<uint32_t *>(p), f);
+            if (t + 4 <= last)
+                *reinterpret_cast<uint32_t *>(p) = u;
+            else
+                for (int k = 0; t + k < last; ++k) p[k] = (uint8_t)(u >> (8 * k));
+        }
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < (m1 - m0) * words; w += 128) {
+        const int m = m0 + w / words, from = src[m], to = dst[m] - block * s.N;
+        const uint8_t *there = s.pool + (int64_t)s.table[table_entry(s, q.seq, from / s.N, head)] * s.page_bytes;
+        const int r = from % s.N, c = w % words;
+        const uint32_t k = *(reinterpret_cast<const uint32_t *>(there + (int64_t)(r / kKvGranule) * (2 * kKvGranule * D) + (r % kKvGranule) * D) + c);
+        *(reinterpret_cast<uint32_t *>(page + (int64_t)(to / kKvGranule) * (2 * kKvGranule * D) + (to % kKvGranule) * D) + c) =
+            shift_codes(k, shift_factor((int)(int16_t)(ex[m] & 0xffff), now[0]));
+        const float f = shift_factor(ex[m] >> 16, now[1]);
+        const uint8_t *v = there + (int64_t)(r / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + r % kKvGranule;
+        uint8_t *o = page + (int64_t)(to / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + to % kKvGranule;
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4) {
+            const int d = c + k4 * words;
+            o[d * kKvGranule] = (uint8_t)shift_codes(v[d * kKvGranule], f);
+        }
+    }
+    if (threadIdx.x == 0) {
+        s.exps[2 * entry] = (int8_t)now[0];
+        s.exps[2 * entry + 1] = (int8_t)now[1];
+    }
+}
+
+int32_t check_launch(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SLORA_OK : fail(SLORA_EHIP, "launching %s: %s", what, hipGetErrorString(e));
+}
+
+// f(integral constants of the type and of D / 32)
+template <typename F>
+int32_t by_shape(int dtype, int D, F f)
+{
+    auto of = [&](auto dt) -> int32_t {
+        switch (D / 32) {
+        case 1: return f(dt, std::integral_constant<int, 1>{});
+        case 2: return f(dt, std::integral_constant<int, 2>{});
+        case 3: return f(dt, std::integral_constant<int, 3>{});
+        case 4: return f(dt, std::integral_constant<int, 4>{});
+        case 6: return f(dt, std::integral_constant<int, 6>{});
+        case 8: return f(dt, std::integral_constant<int, 8>{});
+        }
+        return fail(SLORA_EINVAL, "no kernel for head_dim=%d", D);
+    };
+    return dtype == SLORA_F16 ? of(std::integral_constant<int, SLORA_F16>{}) : of(std::integral_constant<int, SLORA_BF16>{});
+}
+
+} // namespace
+
+int32_t launch_kv_table(const slora_kv8_batch *b, void *stream)
+{
+    hipLaunchKernelGGL(kv_table_kernel, dim3((unsigned)b->columns.size()), dim3(256), 0, (hipStream_t)stream, b->cache->d_table, b->d_columns, b->d_pages,
+                       b->cache->per_block());
+    return check_launch("kv_table");
+}
+
+int32_t launch_kv_append(const slora_kv8_batch *b, const KvShape &shape, const KvAppend &a, void *stream)
+{
+    if (b->append.empty()) return SLORA_OK;
+    const dim3 grid((unsigned)(b->append.size() * shape.n_kv)), block(2 * kWave);
+    if (b->cache->pool->dtype == SLORA_F16)
+        hipLaunchKernelGGL(kv_append_kernel<SLORA_F16>, grid, block, 0, (hipStream_t)stream, b->d_append, b->d_seqs, shape, a);
+    else
+        hipLaunchKernelGGL(kv_append_kernel<SLORA_BF16>, grid, block, 0, (hipStream_t)stream, b->d_append, b->d_seqs, shape, a);
+    return check_launch("kv_append");
+}
+
+int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, void *stream)
+{
+    return by_shape(b->cache->pool->dtype, shape.D, [&](auto dt, auto db) {
+        hipLaunchKernelGGL((kv_attend_few_kernel<dt.value, db.value>), dim3((unsigned)(b->attend.size() * shape.n_kv)), dim3(kKvFewThreads), 0,
+                           (hipStream_t)stream, b->d_attend, b->d_seqs, shape, a);
+        int32_t rc = check_launch("kv_attend");
+        if (rc == SLORA_OK && !b->join.empty()) {
+            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv)), dim3(256), 0, (hipStream_t)stream,
+                               b->d_join, b->d_seqs, shape, a);
+            rc = check_launch("kv_join");
+        }
+        return rc;
+    });
+}
+
+int32_t launch_kv_weights(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, const KvWeights &w, void *stream)
+{
+    if (b->longest == 0) return SLORA_OK;
+    const int per = kKvFewThreads / kWave * kKvChunk;
+    const dim3 grid((unsigned)((b->longest + per - 1) / per), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
+    return by_shape(b->cache->pool->dtype, shape.D, [&](auto dt, auto db) {
+        hipLaunchKernelGGL((kv_weights_kernel<dt.value, db.value>), grid, dim3(kKvFewThreads), 0, (hipStream_t)stream, b->d_seqs, shape, a, w);
+        return check_launch("kv_weights");
+    });
+}
+
+int32_t launch_kv_evict(const slora_kv8_batch *b, const KvShape &shape, const KvEvict &e, void *stream)
+{
+    hipLaunchKernelGGL(kv_evict_select_kernel, dim3((unsigned)(b->seqs.size() * shape.n_kv)), dim3(kEvictThreads), 0, (hipStream_t)stream, b->d_seqs, shape, e);
+    int32_t rc = check_launch("kv_evict_select");
+    if (rc == SLORA_OK && b->dest_blocks > 0) {
+        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)b->dest_blocks, (unsigned)shape.n_kv, (unsigned)b->seqs.size()), dim3(128), 0,
+                           (hipStream_t)stream, b->d_seqs, shape, e);
+        rc = check_launch("kv_evict_move");
+    }
+    return rc;
+}
+
+} // namespace slora

@@ -433,6 +433,7 @@ int32_t slora_pool_destroy(slora_pool *pool)
     clear_error();
     if (!pool) return SLORA_OK;
     if (pool->live_plans) return fail(SLORA_EBUSY, "%lld plan(s) of this pool still exist", (long long)pool->live_plans);
+    if (pool->live_caches) return fail(SLORA_EBUSY, "%lld KV cache(s) of this pool still exist", (long long)pool->live_caches);
     if (pool->dev_base) {
         DeviceScope dev(pool->device);
         (void)hipDeviceSynchronize();

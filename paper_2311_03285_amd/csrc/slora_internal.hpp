@@ -200,6 +200,7 @@ struct slora_pool {
     int64_t n_free = 0;
     uint64_t unload_generation = 0;
     int64_t live_plans = 0;
+    int64_t live_caches = 0;                          // 8-bit KV caches on its pages
     int64_t mfma_min_tokens = 16;
     int64_t mfma_min_tiles = 32;
     int64_t xcd_group = 0;                            // accepted, no effect

@@ -19,6 +19,7 @@ MAX_MULTI = 8
 STATIC_SCRATCH_BYTES = 64 << 20
 PLAN_INFO_N = 13
 POOL_STATS_N = 4
+KV8_INFO_N = 4
 PLAN_INFO_KEYS = ("tokens", "groups", "groups_vec", "groups_mfma", "vec_shrink_items", "vec_expand_items",
                   "mfma_shrink_items", "mfma_expand_items", "v_stride", "sum_rank", "split_tiles",
                   "scratch_bytes_per_slot", "groups_fused")
@@ -74,6 +75,22 @@ def lib() -> C.CDLL:
             "slora_lora_expand": (i32, [vp, i32, vp, vp, vp]),
             "slora_lora_shrink_expand": (i32, [vp, i32, vp, vp, vp, i32, i32, vp, vp]),
             "slora_set_option": (i32, [vp, C.c_char_p, i64]),
+            "slora_kv8_init": (i32, [C.POINTER(vp), vp, i32, i32, i32, i32, i32, i32, vp]),
+            "slora_kv8_destroy": (i32, [vp]),
+            "slora_kv8_info": (i32, [vp, vp, i32]),
+            "slora_kv8_lengths": (i32, [vp, i32, vp, vp]),
+            "slora_kv8_extend": (i32, [vp, i32, vp, vp, vp, i64]),
+            "slora_kv8_truncate": (i32, [vp, i32, vp, vp, i32]),
+            "slora_kv8_batch_plan": (i32, [vp, C.POINTER(vp), i32, vp, vp, vp]),
+            "slora_kv8_batch_destroy": (i32, [vp]),
+            "slora_kv8_append": (i32, [vp, i32, vp, i64, vp, i64, vp]),
+            "slora_kv8_attend": (i32, [vp, i32, vp, i64, vp, i64, C.c_float, i32, vp, vp, vp, vp]),
+            "slora_kv8_evict": (i32, [vp, i32, i32, vp, vp, vp, vp, vp]),
+            "slora_w4_bytes": (i32, [i32, i32, i32, vp]),
+            "slora_w4_pack": (i32, [C.POINTER(vp), i32, i32, i32, i32, vp, vp, vp, vp, vp]),
+            "slora_w4_destroy": (i32, [vp]),
+            "slora_w4_matmul": (i32, [i32, vp, vp, i32, vp, vp]),
+            "slora_w4_matmul_y16": (i32, [i32, vp, vp, i32, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -270,3 +287,125 @@ def lora_shrink_expand(pool, slot: int, x: int, token_adapter_ids, seg_offsets, 
 
 def set_option(pool, key: str, value: int) -> None:
     _check(lib().slora_set_option(pool, key.encode(), value))
+
+
+# ---- the KV cache in 8 bits ------------------------------------------------------------------
+def _same_length(seqs, **others):
+    for name, a in others.items():
+        if a.size != seqs.size:
+            raise ValueError(f"{name} has {a.size} entries for {seqs.size} sequences")
+
+
+def kv8_init(pool, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, max_seqs: int, max_tokens: int,
+             dev_exps: Optional[int]) -> C.c_void_p:
+    """dev_exps: address of max_seqs * blocks * n_layers * n_kv_heads * 2 device bytes (blocks: kv8_block_count)."""
+    h = C.c_void_p()
+    _check(lib().slora_kv8_init(C.byref(h), pool, n_layers, n_heads, n_kv_heads, head_dim, max_seqs, max_tokens, dev_exps or None))
+    return h
+
+
+def kv8_block_count(page_H: int, head_dim: int, tokens: int) -> int:
+    """Blocks (pages per layer and head) of that many tokens."""
+    block = 8 * (page_H // (8 * head_dim))
+    return -(-tokens // block)
+
+
+def kv8_destroy(cache) -> None:
+    _check(lib().slora_kv8_destroy(cache))
+
+
+def kv8_info(cache) -> dict:
+    out = np.zeros(KV8_INFO_N, dtype=np.int64)
+    _check(lib().slora_kv8_info(cache, _ptr(out), KV8_INFO_N))
+    return dict(zip(("block", "max_blocks", "pages_per_block", "pages"), (int(v) for v in out)))
+
+
+def kv8_lengths(cache, seqs) -> np.ndarray:
+    s = _i32(seqs)
+    out = np.zeros(max(s.size, 1), dtype=np.int32)
+    _check(lib().slora_kv8_lengths(cache, s.size, _ptr(s), _ptr(out)))
+    return out[:s.size]
+
+
+def kv8_extend(cache, seqs, tokens, page_idx=None) -> None:
+    """Room for tokens[i] more tokens in seqs[i], on pages of the library's choice or on page_idx [i][block][layer][head]."""
+    s, t = _i32(seqs), _i32(tokens)
+    _same_length(s, tokens=t)
+    p = None if page_idx is None else _i32(page_idx).reshape(-1)
+    _check(lib().slora_kv8_extend(cache, s.size, _ptr(s), _ptr(t), _ptr(p), 0 if p is None else p.size))
+
+
+def kv8_truncate(cache, seqs, lengths, evicted: bool = False) -> None:
+    s, t = _i32(seqs), _i32(lengths)
+    _same_length(s, lengths=t)
+    _check(lib().slora_kv8_truncate(cache, s.size, _ptr(s), _ptr(t), 1 if evicted else 0))
+
+
+def kv8_batch_plan(cache, seqs, rows, keep=None) -> C.c_void_p:
+    s, r = _i32(seqs), _i32(rows)
+    k = None if keep is None else _i32(keep)
+    _same_length(s, rows=r, **({} if k is None else {"keep": k}))
+    h = C.c_void_p()
+    _check(lib().slora_kv8_batch_plan(cache, C.byref(h), s.size, _ptr(s), _ptr(r), _ptr(k)))
+    return h
+
+
+def kv8_batch_destroy(batch) -> None:
+    _check(lib().slora_kv8_batch_destroy(batch))
+
+
+def kv8_append(batch, layer: int, k: int, k_stride: int, v: int, v_stride: int, stream=None) -> None:
+    """k, v: device addresses; strides between rows in elements."""
+    _check(lib().slora_kv8_append(batch, layer, k or None, k_stride, v or None, v_stride, _stream(stream)))
+
+
+def kv8_attend(batch, layer: int, q: int, q_stride: int, out: int, out_stride: int, scale: float, causal: bool = True,
+               weights=None, stream=None) -> None:
+    """weights: None, or the addresses (weights_in, weights_out, pos)."""
+    w_in, w_out, pos = weights or (None, None, None)
+    _check(lib().slora_kv8_attend(batch, layer, q or None, q_stride, out or None, out_stride, scale, 1 if causal else 0,
+                                  w_in, w_out, pos, _stream(stream)))
+
+
+def kv8_evict(batch, layer: int, recent: int, weights_in: int, weights_out: int, pos_in: int, pos_out: int, stream=None) -> None:
+    _check(lib().slora_kv8_evict(batch, layer, recent, weights_in or None, weights_out or None, pos_in or None, pos_out or None,
+                                 _stream(stream)))
+
+
+# ---- products with 4-bit weights ---------------------------------------------------------------
+def w4_bytes(outputs: int, inputs: int, group: int) -> int:
+    """Device bytes of a packed matrix."""
+    out = np.zeros(1, dtype=np.int64)
+    _check(lib().slora_w4_bytes(outputs, inputs, group, _ptr(out)))
+    return int(out[0])
+
+
+def w4_pack(outputs: int, inputs: int, group: int, dtype: int, codes: int, scales: int, zeros: Optional[int], packed: int,
+            stream=None) -> C.c_void_p:
+    """Device addresses; `packed` is borrowed until w4_destroy."""
+    h = C.c_void_p()
+    _check(lib().slora_w4_pack(C.byref(h), outputs, inputs, group, dtype, codes or None, scales or None, zeros or None, packed or None,
+                               _stream(stream)))
+    return h
+
+
+def w4_destroy(w) -> None:
+    _check(lib().slora_w4_destroy(w))
+
+
+def _handle_array(handles):
+    return (C.c_void_p * len(handles))(*[getattr(h, "value", h) for h in handles])
+
+
+def w4_matmul(handles, xs: Sequence[int], T: int, ys: Sequence[int], stream=None) -> None:
+    """ys[k] = xs[k] W_k in fp32."""
+    if not len(handles) == len(xs) == len(ys):
+        raise ValueError("as many xs and ys as matrices")
+    _check(lib().slora_w4_matmul(len(handles), _handle_array(handles), _ptr_array(xs), T, _ptr_array(ys), _stream(stream)))
+
+
+def w4_matmul_y16(handles, xs: Sequence[int], T: int, ys: Sequence[int], stream=None) -> None:
+    """... in the matrices' 16-bit type."""
+    if not len(handles) == len(xs) == len(ys):
+        raise ValueError("as many xs and ys as matrices")
+    _check(lib().slora_w4_matmul_y16(len(handles), _handle_array(handles), _ptr_array(xs), T, _ptr_array(ys), _stream(stream)))
