@@ -386,7 +386,7 @@ typedef struct slora_kv8 slora_kv8;             /* a cache: page table, lengths 
 typedef struct slora_kv8_batch slora_kv8_batch; /* one batch's work lists and scratch */
 
 /*
- * A cache for up to max_seqs sequences of up to max_tokens tokens in each of n_layers layers, on pages
+ * A cache for up to max_seqs sequences of up to max_tokens <= 2^27 tokens in each of n_layers layers, on pages
  * of `pool`.  n_heads query heads share n_kv_heads heads of K and V (n_heads % n_kv_heads == 0);
  * head_dim is 32, 64, 96, 128, 192 or 256 and at most page_H / 8.  dev_exps: DEVICE memory of the caller
  * (borrowed like the pool's), max_seqs * ceil(max_tokens / N) * n_layers * n_kv_heads * 2 bytes: the

@@ -203,7 +203,7 @@ int32_t slora_kv8_init(slora_kv8 **out, slora_pool *pool, int32_t n_layers, int3
         return fail(SLORA_EINVAL, "head_dim=%d must be 32, 64, 96, 128, 192 or 256", head_dim);
     if (pool->H < 8 * head_dim) return fail(SLORA_EINVAL, "a page of H=%d holds fewer than 8 tokens of head_dim=%d", pool->H, head_dim);
     if (max_seqs < 1 || max_seqs > 65535) return fail(SLORA_EINVAL, "max_seqs=%d must be in [1, 65535]", max_seqs);
-    if (max_tokens < 1 || max_tokens > 1 << 30) return fail(SLORA_EINVAL, "max_tokens=%d must be in [1, 2^30]", max_tokens);
+    if (max_tokens < 1 || max_tokens > 1 << 27) return fail(SLORA_EINVAL, "max_tokens=%d must be in [1, 2^27]", max_tokens);
     if (pool->dev_base && !dev_exps) return fail(SLORA_EINVAL, "dev_exps is NULL");
     slora_kv8 *c = new (std::nothrow) slora_kv8;
     if (!c) return fail(SLORA_ENOMEM, "out of host memory");

@@ -38,7 +38,7 @@ __device__ __forceinline__ uint16_t narrow(float f)
 __device__ __forceinline__ float across_16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float across_32(float v) { return __shfl_xor(v, 32, kWave); }
 
-// n / (granules per block) for n < 2^17 or so many: div = ceil(2^32 / d) is exact while n * d < 2^32; 0 stands for d = 1
+// n / (granules per block) by div = ceil(2^32 / d): exact while n * d < 2^32, and n < 2^24 granules, d <= 128; 0 stands for d = 1
 __device__ __forceinline__ uint32_t kv_div(uint32_t n, uint32_t div) { return div ? __umulhi(n, div) : n; }
 
 __device__ __forceinline__ int64_t table_entry(const KvShape &s, int seq, int block, int head)
@@ -553,8 +553,6 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_weights_kernel(const KvSeq *
 // ---------------------------------------------------------------------------------------
 // eviction
 // ---------------------------------------------------------------------------------------
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
-
 // numbers in the order of the weights: recent tokens above everything, then NaN, then values; -0 is 0
 __device__ __forceinline__ uint32_t rank_of(float w, int32_t pos, int32_t recent_from)
 {
@@ -564,20 +562,50 @@ __device__ __forceinline__ uint32_t rank_of(float w, int32_t pos, int32_t recent
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per sequence and head.  The rank of the last token that stays is found eight bits at a time; then every wavefront takes
-// a run of slots, and counts say where its places and moves go in the lists: all integers, in the order of the slots.
-__global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
+// What the wavefronts of a team wait for: all of a workgroup, or the lanes of one wavefront (whose LDS operations are in order)
+template <int W>
+__device__ __forceinline__ void team_sync()
 {
-    __shared__ uint32_t bins[256];
-    __shared__ uint32_t found[2];
-    __shared__ int counts[3][kEvictWaves];
-    const KvSeq q = seqs[blockIdx.x / s.n_kv];
-    const int head = blockIdx.x % s.n_kv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if constexpr (W > 1) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    }
+}
+
+// A team of W wavefronts per sequence and head; a wavefront has a run of slots, 64 of them a stripe.  Ranks are kept in LDS, `held` of each
+// wavefront's (longer runs are ranked again).  The rank of the last token that stays is found BITS bits at a time: bins are counted in
+// LDS, and every wavefront finds the digit from the counts for itself - lane l has the bins of digits B l .. B l + B - 1, digit B l + k
+// at place 64 k + l.  Then the counts of each run say where its places and moves go in the lists: all
+// integers, in the order of the slots.
+template <int W>
+struct Evict {
+    static constexpr int kThreads = W == 1 ? 256 : W * kWave, kTeams = kThreads / kWave / W;
+    static constexpr int kBits = W < 16 ? 8 : 11, kBins = 1 << kBits, kPer = kBins / kWave;
+    static constexpr int kHeld = W == 1 ? 1536 : 2048; // ranks of each wavefront: at most 33 and 145 KiB a workgroup
+    static constexpr unsigned lds(int held) { return (unsigned)(kTeams * (W * held + 2 * kBins + 4 * W) * 4); }
+};
+
+template <int W>
+__global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(const KvSeq *__restrict__ seqs, int n_rows, int held, KvShape s, KvEvict e)
+{
+    constexpr int kTeams = Evict<W>::kTeams, kBits = Evict<W>::kBits, kBins = Evict<W>::kBins, kPer = Evict<W>::kPer;
+    extern __shared__ uint32_t lds[];
+    const int team = threadIdx.x / kWave / W, wave = threadIdx.x / kWave % W, lane = threadIdx.x % kWave;
+    const int row = blockIdx.x * kTeams + team;
+    if (row >= n_rows) return; // (a whole team; teams of one wavefront do not wait for each other)
+    uint32_t *mine_lds = lds + team * (W * held + 2 * kBins + 4 * W);
+    uint32_t *bins = mine_lds, *counts = bins + 2 * kBins, *ranks = counts + 4 * W + wave * held;
+    const KvSeq q = seqs[row / s.n_kv];
+    const int head = row % s.n_kv;
     const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens;
     const float *w = e.w_in + at;
     const int32_t *pos = e.pos_in + at;
+    const bool copies = e.w_out != e.w_in || e.pos_out != e.pos_in;
     if (q.keep >= q.len) {
-        for (int i = threadIdx.x; i < q.len; i += kEvictThreads) {
+        for (int i = wave * kWave + lane; copies && i < q.len; i += W * kWave) {
             e.w_out[at + i] = w[i];
             e.pos_out[at + i] = pos[i];
         }
@@ -585,169 +613,271 @@ __global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const Kv
     }
     if (q.keep == 0) return;
     const int recent_from = q.seen - min(min(e.recent, q.keep), q.seen);
-    // the rank of the keep-th token, and how many of that rank stay
-    uint32_t prefix = 0;
-    int left = q.keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (threadIdx.x < 256) bins[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < q.len; i += kEvictThreads) {
-            const uint32_t r = rank_of(w[i], pos[i], recent_from);
-            if (shift == 24 || (r >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[(r >> shift) & 255u], 1u);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            int k = 255;
-            uint32_t above = 0;
-            while (k > 0 && above + bins[k] < (uint32_t)left) above += bins[k--];
-            found[0] = (uint32_t)k;
-            found[1] = above;
-        }
-        __syncthreads();
-        prefix |= found[0] << shift;
-        left -= (int)found[1];
-        __syncthreads();
-    }
-    // slots of this wavefront
-    const int run = ((q.len + kEvictWaves - 1) / kEvictWaves + kWave - 1) / kWave * kWave;
-    const int lo = wave * run, hi = min(lo + run, q.len);
-    auto before = [&](const int (&c)[kEvictWaves]) {
-        int b = 0;
-        for (int k = 0; k < wave; ++k) b += c[k];
-        return b;
-    };
-    int equal = 0;
-    for (int i = lo + lane; i - lane < hi; i += kWave) equal += __popcll(__ballot(i < hi && rank_of(w[i], pos[i], recent_from) == prefix));
-    if (lane == 0) counts[0][wave] = equal;
-    __syncthreads();
-    const int equal_before = before(counts[0]);
-    const uint64_t lower = (uint64_t(1) << lane) - 1;
-    // calls f(slot, stays) for 64 slots at a time
+    const int run = ((q.len + W - 1) / W + kWave - 1) / kWave * kWave;
+    const int lo = wave * run, n = max(min(run, q.len - lo), 0); // slots [lo, lo + n)
+    // calls f(slot, rank, whether there is such a slot) for the stripes in turn; the lanes stay together
     auto walk = [&](auto f) {
-        int seen = equal_before;
-        for (int i = lo + lane; i - lane < hi; i += kWave) {
-            const uint32_t r = i < hi ? rank_of(w[i], pos[i], recent_from) : 0;
-            const uint64_t same = __ballot(i < hi && r == prefix);
-            f(i, i < hi && (r > prefix || (r == prefix && seen + (int)__popcll(same & lower) < left)));
-            seen += __popcll(same);
+        const int some = min(n, held);
+        constexpr int kAhead = 4;
+        for (int j0 = 0; j0 < some; j0 += kAhead * kWave) {
+            uint32_t r[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) r[k] = ranks[min(j0 + k * kWave, held - kWave) + lane];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int j = j0 + k * kWave;
+                if (j < some) f(lo + j + lane, r[k], j + lane < n);
+            }
+        }
+        for (int j = held; j < n; j += kWave) {
+            const bool in = j + lane < n;
+            f(lo + j + lane, in ? rank_of(w[lo + j + lane], pos[lo + j + lane], recent_from) : 0, in);
         }
     };
-    int holes = 0, moves = 0;
-    walk([&](int i, bool stays) {
-        holes += __popcll(__ballot(i < hi && i < q.keep && !stays));
-        moves += __popcll(__ballot(i < hi && i >= q.keep && stays));
-    });
-    if (lane == 0) {
-        counts[1][wave] = holes;
-        counts[2][wave] = moves;
-    }
-    __syncthreads();
-    holes = before(counts[1]);
-    moves = before(counts[2]);
-    int total = 0;
-    for (int k = 0; k < kEvictWaves; ++k) total += counts[2][k];
-    const int most = min(q.keep, q.len - q.keep), blocks = (q.keep + s.N - 1) / s.N;
-    int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
-    int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
-    walk([&](int i, bool stays) {
-        const bool hole = i < hi && i < q.keep && !stays, move = i < hi && i >= q.keep && stays;
-        const uint64_t hs = __ballot(hole), ms = __ballot(move);
-        const int h = holes + __popcll(hs & lower);
-        if (i < hi && i < q.keep && i % s.N == 0) first[i / s.N] = h;
-        if (hole) dst[h] = i;
-        if (move) {
-            const int m = moves + __popcll(ms & lower);
-            src[m] = i;
-            const int16_t both = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, i / s.N, head)];
-            ex[m] = (int32_t)(int8_t)(both & 0xff) & 0xffff;
-            ex[m] |= (int32_t)(both >> 8) << 16;
+    auto place = [](uint32_t digit) { return (digit % kPer) * kWave + digit / kPer; };
+    auto count = [&](uint32_t *now, uint32_t digit, bool yes) { // many lanes of one digit: one of them for all
+        const uint64_t live = __ballot(yes);
+        if (live == 0) return;
+        const uint32_t d0 = (uint32_t)__builtin_amdgcn_readlane((int)digit, (int)__ffsll((unsigned long long)live) - 1);
+        const uint64_t same = __ballot(yes && digit == d0);
+        if (same == live) {
+            if (lane == 0) atomicAdd(&now[place(d0)], (uint32_t)__popcll(live));
+        } else if (yes) {
+            atomicAdd(&now[place(digit)], 1u);
         }
-        holes += __popcll(hs);
-        moves += __popcll(ms);
-    });
-    if (threadIdx.x == 0) first[blocks] = total;
-    __syncthreads();
-    // (entries of slots from keep on are only read)
-    for (int i = threadIdx.x; i < total; i += kEvictThreads) {
-        e.w_out[at + dst[i]] = w[src[i]];
-        e.pos_out[at + dst[i]] = pos[src[i]];
-    }
-    if (e.w_out != e.w_in || e.pos_out != e.pos_in) {
-        // the places that are not in the list, between those that are
-        for (int k = threadIdx.x / kWave; k <= total; k += kEvictWaves) {
-            const int from = k ? dst[k - 1] + 1 : 0, to = k < total ? dst[k] : q.keep;
-            for (int i = from + lane; i < to; i += kWave) {
-                if (e.w_out != e.w_in) e.w_out[at + i] = w[i];
-                if (e.pos_out != e.pos_in) e.pos_out[at + i] = pos[i];
+    };
+
+    for (int k = wave * kWave + lane; k < kBins; k += W * kWave) bins[k] = 0;
+    team_sync<W>();
+    // ranks, and the counts of their first bits; eight stripes are loaded together
+    constexpr int kAhead = 8;
+    for (int j = 0; j < n; j += kAhead * kWave) {
+        float a[kAhead];
+        int32_t p[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = min(j + k * kWave + lane, n - 1) + lo;
+            a[k] = w[i];
+            p[k] = pos[i];
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = j + k * kWave + lane;
+            const uint32_t r = rank_of(a[k], p[k], recent_from);
+            if (i - lane < held && i - lane < n) ranks[i] = r;
+            count(bins, r >> (32 - kBits), i < n);
+            if (copies && i < n && lo + i < q.keep) { // (places that fall free are written again, by what moves there)
+                e.w_out[at + lo + i] = a[k];
+                e.pos_out[at + lo + i] = p[k];
             }
         }
     }
+    // the rank of the keep-th token, and how many of that rank stay
+    uint32_t prefix = 0;
+    int left = q.keep;
+    int turn = 0;
+#pragma unroll 1
+    for (int top = 32; top > 0; top -= kBits, turn ^= 1) {
+        const int shift = max(top - kBits, 0);
+        uint32_t *now = bins + turn * kBins, *next = bins + (turn ^ 1) * kBins;
+        if (top < 32) {
+            const uint32_t mask = (1u << (top - shift)) - 1;
+            walk([&](int, uint32_t r, bool in) { count(now, (r >> shift) & mask, in && (r >> top) == (prefix >> top)); });
+        }
+        if (shift > 0)
+            for (int k = wave * kWave + lane; k < kBins; k += W * kWave) next[k] = 0;
+        team_sync<W>();
+        uint32_t c[kPer], mine = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) mine += c[k] = now[k * kWave + lane];
+        uint32_t from = mine; // what this lane and those above it count
+#pragma unroll
+        for (int x = 1; x < kWave; x *= 2) {
+            const uint32_t other = (uint32_t)__shfl_down((int)from, x, kWave);
+            if (lane + x < kWave) from += other;
+        }
+        uint32_t above = from - mine;
+        const int owner = 63 - (int)__clzll((long long)__ballot(from >= (uint32_t)left)); // the highest lane with enough
+        int found = kPer - 1;
+#pragma unroll
+        for (int k = kPer - 1; k > 0; --k) {
+            if (found == k && above + c[k] < (uint32_t)left) {
+                above += c[k];
+                found = k - 1;
+            }
+        }
+        prefix |= (uint32_t)__builtin_amdgcn_readlane(kPer * lane + found, owner) << shift;
+        left -= __builtin_amdgcn_readlane((int)above, owner);
+        uint32_t there = c[0];
+#pragma unroll
+        for (int k = 1; k < kPer; ++k) there = found == k ? c[k] : there;
+        if (shift > 0 && prefix > 0 && __builtin_amdgcn_readlane((int)there, owner) == left) { // all of this digit stay: everything above prefix - 1
+            prefix -= 1;
+            left = 0;
+            break;
+        }
+    }
+
+    // where this run's places and moves go: from what the runs before it have, tokens of greater and of equal rank before and from keep on
+    int seen = 0, holes = 0, moves = 0, total = 0; // equal ranks, places, moves so far; all moves
+    if constexpr (W > 1) {
+        int c[4] = {0, 0, 0, 0}; // greater and equal before keep, then from keep on
+        walk([&](int i, uint32_t r, bool in) {
+            const int g = in && r > prefix, same = in && r == prefix, before = i < q.keep;
+            c[0] += g & before;
+            c[1] += same & before;
+            c[2] += g & ~before;
+            c[3] += same & ~before;
+        });
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int x = 32; x; x >>= 1) c[k] += __shfl_xor(c[k], x, kWave);
+            if (lane == 0) counts[k * W + wave] = (uint32_t)c[k];
+        }
+        team_sync<W>();
+        int all_seen = 0, all_holes = 0;
+        for (int k = 0; k < W; ++k) {
+            if (k == wave) seen = all_seen, holes = all_holes, moves = total;
+            const int e0 = (int)counts[W + k], e1 = (int)counts[3 * W + k];
+            const int stay0 = max(min(left - all_seen, e0), 0), stay1 = max(min(left - all_seen - e0, e1), 0);
+            all_holes += max(min(q.keep - k * run, min(run, q.len - k * run)), 0) - (int)counts[k] - stay0;
+            total += (int)counts[2 * W + k] + stay1;
+            all_seen += e0 + e1;
+        }
+    }
+    const uint64_t lower = (uint64_t(1) << lane) - 1;
+    const int most = min(q.keep, q.len - q.keep), blocks = (q.keep + s.N - 1) / s.N;
+    int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
+    int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
+    walk([&](int i, uint32_t r, bool in) {
+        const uint64_t same = __ballot(in && r == prefix);
+        const bool stays = in && (r > prefix || (r == prefix && seen + (int)__popcll(same & lower) < left));
+        seen += (int)__popcll(same);
+        if (i - lane < q.keep) { // (a stripe about keep has both)
+            const bool hole = in && i < q.keep && !stays;
+            const uint64_t hs = __ballot(hole);
+            const int h = holes + (int)__popcll(hs & lower);
+            if (in && i < q.keep && i % kKvGranule == 0) {
+                const int b = (int)kv_div((uint32_t)i / kKvGranule, s.div_b);
+                if (b * s.N == i) first[b] = h;
+            }
+            if (hole) dst[h] = i;
+            holes += (int)__popcll(hs);
+        }
+        const bool move = i >= q.keep && stays;
+        const uint64_t ms = __ballot(move);
+        if (move) {
+            const int m = moves + (int)__popcll(ms & lower);
+            src[m] = i;
+            const int16_t both = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, i / s.N, head)];
+            ex[m] = ((int32_t)(int8_t)(both & 0xff) & 0xffff) | ((int32_t)(both >> 8) << 16);
+        }
+        moves += (int)__popcll(ms);
+    });
+    if constexpr (W == 1) total = moves;
+    if (wave == 0 && lane == 0) first[blocks] = total;
+    team_sync<W>();
+    // (entries of slots from keep on are only read)
+    for (int m = wave * kWave + lane; m < total; m += W * kWave) {
+        e.w_out[at + dst[m]] = w[src[m]];
+        e.pos_out[at + dst[m]] = pos[src[m]];
+    }
 }
 
-// One workgroup per block that keeps tokens, and head.  Nobody writes slots from keep on, and nobody else this block's.
-__global__ __launch_bounds__(128) void kv_evict_move_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
+// A workgroup = some of the blocks of a row (sequence and head) that keep tokens, those that take any.  Nobody writes slots from keep on,
+// and nobody else these blocks'.  A thread has 16 bytes of a token's K, or the eight tokens of a granule in one element
+// of V: what stays (shifted, if a larger exponent comes) and what comes are put together in registers.
+constexpr int kMoveThreads = 256;
+__global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
 {
-    const KvSeq q = seqs[blockIdx.z];
-    const int head = blockIdx.y, block = blockIdx.x, D = s.D;
+    // of each slot of the block (a page holds at most 32768 / 32 tokens): where its token comes from, as the address of element 0 of K; V's
+    // is behind.  Its own place, if it stays.
+    __shared__ const uint8_t *from_k[1024], *from_v[1024];
+    __shared__ float factor[2][1024];
+    __shared__ __align__(8) uint8_t comes[1024];
+    const KvSeq q = seqs[blockIdx.x / s.n_kv];
+    if (q.keep >= q.len) return;
+    const int head = blockIdx.x % s.n_kv, D = s.D, lane = threadIdx.x % kWave;
     const int blocks = (q.keep + s.N - 1) / s.N;
-    if (q.keep >= q.len || block >= blocks) return;
     const int most = min(q.keep, q.len - q.keep);
     const int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
     const int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
-    const int m0 = first[block], m1 = first[block + 1];
-    if (m0 == m1) return;
-    const int64_t entry = table_entry(s, q.seq, block, head);
-    uint8_t *page = s.pool + (int64_t)s.table[entry] * s.page_bytes;
-    const int was[2] = {s.exps[2 * entry], s.exps[2 * entry + 1]};
-    int now[2] = {was[0], was[1]};
-    for (int m = m0; m < m1; ++m) {
-        now[0] = max(now[0], (int)(int16_t)(ex[m] & 0xffff));
-        now[1] = max(now[1], ex[m] >> 16);
-    }
-    __syncthreads(); // every thread has read the exponents
-    const int last = min(s.N, q.keep - block * s.N); // slots of the block that stay in use
-    const int words = D / 4;
-    if (now[0] != was[0]) {
-        const float f = shift_factor(was[0], now[0]);
-        for (int w = threadIdx.x; w < last * words; w += 128) {
-            const int t = w / words;
-            uint32_t *p = reinterpret_cast<uint32_t *>(page + (int64_t)(t / kKvGranule) * (2 * kKvGranule * D) + (t % kKvGranule) * D) + w % words;
-            *p = shift_codes(*p, f);
-        }
-    }
-    if (now[1] != was[1]) {
-        const float f = shift_factor(was[1], now[1]);
-        // four slots of an element at a time; a granule that others still read has slots behind `last`
-        for (int w = threadIdx.x; w < (last + 3) / 4 * D; w += 128) {
-            const int quad = w / D, d = w % D, t = quad * 4;
-            uint8_t *p = page + (int64_t)(t / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + d * kKvGranule + t % kKvGranule;
-            const uint32_t u = shift_codes(*reinterpret_cast<uint32_t *>(p), f);
-            if (t + 4 <= last)
-                *reinterpret_cast<uint32_t *>(p) = u;
-            else
-                for (int k = 0; t + k < last; ++k) p[k] = (uint8_t)(u >> (8 * k));
-        }
-    }
-    __syncthreads();
-    for (int w = threadIdx.x; w < (m1 - m0) * words; w += 128) {
-        const int m = m0 + w / words, from = src[m], to = dst[m] - block * s.N;
-        const uint8_t *there = s.pool + (int64_t)s.table[table_entry(s, q.seq, from / s.N, head)] * s.page_bytes;
-        const int r = from % s.N, c = w % words;
-        const uint32_t k = *(reinterpret_cast<const uint32_t *>(there + (int64_t)(r / kKvGranule) * (2 * kKvGranule * D) + (r % kKvGranule) * D) + c);
-        *(reinterpret_cast<uint32_t *>(page + (int64_t)(to / kKvGranule) * (2 * kKvGranule * D) + (to % kKvGranule) * D) + c) =
-            shift_codes(k, shift_factor((int)(int16_t)(ex[m] & 0xffff), now[0]));
-        const float f = shift_factor(ex[m] >> 16, now[1]);
-        const uint8_t *v = there + (int64_t)(r / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + r % kKvGranule;
-        uint8_t *o = page + (int64_t)(to / kKvGranule) * (2 * kKvGranule * D) + kKvGranule * D + to % kKvGranule;
+    const int granule_bytes = 2 * kKvGranule * D;
+    // blocks y, y + gridDim.y, ...: 64 at a time
+    for (int k0 = 0; (int)blockIdx.y + k0 * (int)gridDim.y < blocks; k0 += kWave) {
+        const int mine = (int)blockIdx.y + (k0 + lane) * (int)gridDim.y;
+        uint64_t busy = __ballot(mine < blocks && first[mine] < first[mine + 1]);
+        while (busy) {
+            const int block = (int)blockIdx.y + (k0 + (int)__ffsll((unsigned long long)busy) - 1) * (int)gridDim.y;
+            busy &= busy - 1;
+            const int m0 = first[block], m1 = first[block + 1];
+            const int64_t entry = table_entry(s, q.seq, block, head);
+            uint8_t *page = s.pool + (int64_t)s.table[entry] * s.page_bytes;
+            const int was_k = s.exps[2 * entry], was_v = s.exps[2 * entry + 1];
+            int now_k = was_k, now_v = was_v;
+            for (int m = m0 + lane; m < m1; m += kWave) {
+                now_k = max(now_k, (int)(int16_t)(ex[m] & 0xffff));
+                now_v = max(now_v, ex[m] >> 16);
+            }
 #pragma unroll
-        for (int k4 = 0; k4 < 4; ++k4) {
-            const int d = c + k4 * words;
-            o[d * kKvGranule] = (uint8_t)shift_codes(v[d * kKvGranule], f);
+            for (int x = 32; x; x >>= 1) {
+                now_k = max(now_k, __shfl_xor(now_k, x, kWave));
+                now_v = max(now_v, __shfl_xor(now_v, x, kWave));
+            }
+            const int last = min(s.N, q.keep - block * s.N); // slots of the block that stay in use
+            auto granule = [&](const uint8_t *base, int t) { return base + (int64_t)(t / kKvGranule) * granule_bytes; };
+            __syncthreads(); // the block before is done
+            for (int t = threadIdx.x; t < s.N; t += kMoveThreads) {
+                from_k[t] = granule(page, t) + (t % kKvGranule) * D;
+                from_v[t] = granule(page, t) + kKvGranule * D + t % kKvGranule;
+                factor[0][t] = shift_factor(was_k, now_k);
+                factor[1][t] = shift_factor(was_v, now_v);
+                comes[t] = 0;
+            }
+            __syncthreads();
+            for (int m = m0 + (int)threadIdx.x; m < m1; m += kMoveThreads) {
+                const int t = dst[m] - block * s.N, from = src[m], r = from % s.N;
+                const uint8_t *there = granule(s.pool + (int64_t)s.table[table_entry(s, q.seq, from / s.N, head)] * s.page_bytes, r);
+                from_k[t] = there + (r % kKvGranule) * D;
+                from_v[t] = there + kKvGranule * D + r % kKvGranule;
+                factor[0][t] = shift_factor((int)(int16_t)(ex[m] & 0xffff), now_k);
+                factor[1][t] = shift_factor(ex[m] >> 16, now_v);
+                comes[t] = 1;
+            }
+            __syncthreads();
+            const int chunks = D / 16;
+            for (int u = threadIdx.x; u < last * chunks; u += kMoveThreads) {
+                const int t = u / chunks;
+                if (!comes[t] && now_k == was_k) continue;
+                const u32x4 c = *(reinterpret_cast<const u32x4 *>(from_k[t]) + u % chunks);
+                u32x4 r;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = shift_codes(c[k], factor[0][t]);
+                *(reinterpret_cast<u32x4 *>(page + (int64_t)(t / kKvGranule) * granule_bytes + (t % kKvGranule) * D) + u % chunks) = r;
+            }
+            for (int u = threadIdx.x; u < (last + kKvGranule - 1) / kKvGranule * D; u += kMoveThreads) {
+                const int g = u / D, d = u % D, t0 = g * kKvGranule;
+                if (*reinterpret_cast<const uint64_t *>(&comes[t0]) == 0 && now_v == was_v) continue;
+                uint32_t c[kKvGranule];
+#pragma unroll
+                for (int t = 0; t < kKvGranule; ++t) c[t] = from_v[t0 + t][d * kKvGranule];
+                uint32_t r[2] = {0, 0};
+#pragma unroll
+                for (int t = 0; t < kKvGranule; ++t)
+                    r[t / 4] |= ((uint32_t)(int)__builtin_rintf((float)(int8_t)c[t] * factor[1][t0 + t]) & 0xffu) << (8 * (t % 4));
+                uint8_t *to = page + (int64_t)g * granule_bytes + kKvGranule * D + d * kKvGranule;
+                if (t0 + kKvGranule <= last) {
+                    *reinterpret_cast<u32x2 *>(to) = u32x2{r[0], r[1]};
+                } else { // others may be reading the slots behind
+                    for (int t = 0; t0 + t < last; ++t) to[t] = (uint8_t)(r[t / 4] >> (8 * (t % 4)));
+                }
+            }
+            if (threadIdx.x == 0) { // (everyone has read them: two barriers ago)
+                s.exps[2 * entry] = (int8_t)now_k;
+                s.exps[2 * entry + 1] = (int8_t)now_v;
+            }
         }
-    }
-    if (threadIdx.x == 0) {
-        s.exps[2 * entry] = (int8_t)now[0];
-        s.exps[2 * entry + 1] = (int8_t)now[1];
     }
 }
 
@@ -823,11 +953,27 @@ int32_t launch_kv_weights(const slora_kv8_batch *b, const KvShape &shape, const 
 
 int32_t launch_kv_evict(const slora_kv8_batch *b, const KvShape &shape, const KvEvict &e, void *stream)
 {
-    hipLaunchKernelGGL(kv_evict_select_kernel, dim3((unsigned)(b->seqs.size() * shape.n_kv)), dim3(kEvictThreads), 0, (hipStream_t)stream, b->d_seqs, shape, e);
-    int32_t rc = check_launch("kv_evict_select");
+    const int64_t rows = (int64_t)b->seqs.size() * shape.n_kv;
+    hipStream_t st = (hipStream_t)stream;
+    auto select = [&](auto w) -> int32_t {
+        typedef Evict<w.value> E;
+        // stripes of the longest run, at most what LDS holds
+        const int held = std::min<int>(E::kHeld, ((b->longest + w.value - 1) / w.value + kWave - 1) / kWave * kWave);
+        if (E::lds(held) > 65536) {
+            const hipError_t a = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_evict_select_kernel<w.value>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+            if (a != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(a));
+        }
+        hipLaunchKernelGGL(kv_evict_select_kernel<w.value>, dim3((unsigned)((rows + E::kTeams - 1) / E::kTeams)), dim3(E::kThreads), E::lds(held), st,
+                           b->d_seqs, (int)rows, held, shape, e);
+        return check_launch("kv_evict_select");
+    };
+    int32_t rc = b->longest <= 2048 && rows >= 256 ? select(std::integral_constant<int, 1>{})
+                 : b->longest <= 8192              ? select(std::integral_constant<int, 4>{})
+                                                   : select(std::integral_constant<int, 16>{});
     if (rc == SLORA_OK && b->dest_blocks > 0) {
-        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)b->dest_blocks, (unsigned)shape.n_kv, (unsigned)b->seqs.size()), dim3(128), 0,
-                           (hipStream_t)stream, b->d_seqs, shape, e);
+        // eight workgroups for every compute unit
+        const int64_t split = std::max<int64_t>(1, std::min<int64_t>(b->dest_blocks, (2048 + rows - 1) / rows));
+        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)rows, (unsigned)split), dim3(kMoveThreads), 0, st, b->d_seqs, shape, e);
         rc = check_launch("kv_evict_move");
     }
     return rc;

@@ -107,7 +107,7 @@ def test_batches(cache):
 @pytest.mark.parametrize("kw,code", [
     (dict(head_dim=48), slora.EINVAL), (dict(head_dim=128), slora.EINVAL), (dict(n_heads=7), slora.EINVAL), (dict(n_kv=0), slora.EINVAL),
     (dict(n_layers=0), slora.EINVAL), (dict(max_seqs=0), slora.EINVAL), (dict(max_tokens=0), slora.EINVAL),
-    (dict(max_seqs=65535, max_tokens=1 << 30), slora.ERANGE)])
+    (dict(max_tokens=(1 << 27) + 1), slora.EINVAL), (dict(max_seqs=65535, max_tokens=1 << 27), slora.ERANGE)])
 def test_caches_that_cannot_be(cache, kw, code):
     pool, _ = cache
     a = dict(n_layers=1, n_heads=6, n_kv=3, head_dim=64, max_seqs=4, max_tokens=100)
