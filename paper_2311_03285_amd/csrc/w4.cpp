@@ -100,7 +100,7 @@ int32_t matmul(int32_t n, const slora_w4 *const *w, const void *const *x, int32_
             if (y[m] == y[k]) return fail(SLORA_EINVAL, "y[%d] and y[%d] are the same buffer", m, k);
         a.m[k].codes = w[k]->packed;
         a.m[k].scales = reinterpret_cast<const uint16_t *>(w[k]->packed + w[k]->code_bytes());
-        a.m[k].zeros = w[k]->has_zeros ? w[k]->packed + w[k]->code_bytes() + 2 * w[k]->units() : nullptr;
+        a.m[k].zeros = w[k]->packed + w[k]->code_bytes() + 2 * w[k]->units();
         a.m[k].x = static_cast<const uint16_t *>(x[k]);
         a.m[k].y = y[k];
         a.m[k].outputs = w[k]->outputs;

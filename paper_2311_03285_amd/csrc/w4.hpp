@@ -6,7 +6,7 @@
 // Packed matrix.  Tiles of 16 outputs x chunks of 128 inputs, 1 KiB each: lane l = 16 g + r of a wavefront has 16 bytes, word s of
 // them the codes of output r and inputs 32 s + 8 g + i of the chunk, i = 0 .. 3 in the low halves of the four bytes and 4 .. 7 in the high ones.
 // Behind them the scales, 16 per tile, chunk and unit of 32, 64 or 128 inputs (the largest of these that divides
-// the group), then the zeros, one byte each, if there are any.  Outputs and inputs beyond the matrix have scale 0.
+// the group), then the zeros, one byte 0x80 | z each.  Outputs and inputs beyond the matrix have scale 0.
 constexpr int kW4Rows = 16, kW4Chunk = 128;
 
 struct slora_w4 {
@@ -24,7 +24,7 @@ namespace slora {
 struct W4Matrix {
     const uint8_t *codes;
     const uint16_t *scales;
-    const uint8_t *zeros; // NULL: 8
+    const uint8_t *zeros;
     const uint16_t *x;
     void *y;
     int32_t outputs, inputs, chunks;
