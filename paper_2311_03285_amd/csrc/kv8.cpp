@@ -417,6 +417,14 @@ int32_t slora_kv8_batch_plan(slora_kv8 *c, slora_kv8_batch **out, int32_t n, con
                 b->firsts += (int64_t)(c->blocks(s.keep) + 1) * c->n_kv;
                 b->dest_blocks = std::max(b->dest_blocks, c->blocks(s.keep));
             }
+            const int64_t cols = (int64_t)rows[i] * (c->n_heads / c->n_kv);
+            s.score0 = cols <= kKvFewCols ? b->scores : -1;
+            if (cols <= kKvFewCols) {
+                b->scores += cols * c->n_kv * (((int64_t)q.len + 7) / 8 * 8);
+                b->longest_few = std::max(b->longest_few, q.len);
+            } else {
+                b->longest_many = std::max(b->longest_many, q.len);
+            }
             b->seqs.push_back(s);
             b->cuts.push_back((int32_t)q.cuts);
             for (int32_t k = q.on_device; k < c->blocks(q.len); ++k) b->columns.push_back(seqs[i] * c->max_blocks + k);
@@ -504,7 +512,9 @@ int32_t slora_kv8_attend(slora_kv8_batch *b, int32_t layer, const void *q, int64
     if (dev.status() != SLORA_OK) return dev.status();
     const size_t o_floats = (size_t)b->part_cols * c->n_kv * c->D, ml_floats = (size_t)b->part_cols * c->n_kv * 2;
     const size_t stat_floats = (size_t)b->rows * c->n_heads * 2;
-    rc = c->pool->grow_v(b->set, o_floats + ml_floats + stat_floats, 0, stream);
+    // (scores first: their rows are 32-byte aligned)
+    const size_t score_floats = weights ? (size_t)b->scores : 0;
+    rc = c->pool->grow_v(b->set, score_floats + o_floats + ml_floats + stat_floats, 0, stream);
     if (rc == SLORA_OK) rc = b->enter(stream);
     if (rc != SLORA_OK) return rc;
     KvAttend a{};
@@ -514,7 +524,8 @@ int32_t slora_kv8_attend(slora_kv8_batch *b, int32_t layer, const void *q, int64
     a.out_stride = out_stride;
     a.scale = scale * 1.44269504088896340736f;
     a.causal = causal != 0;
-    a.part_o = b->set->v;
+    a.scores = weights ? b->set->v : nullptr;
+    a.part_o = b->set->v + score_floats;
     a.part_ml = a.part_o + o_floats;
     a.stat = a.part_ml + ml_floats;
     const KvShape s = shape_of(c, layer);

@@ -21,8 +21,10 @@ struct KvSeq {
     int32_t keep;      // tokens that an eviction leaves
     int32_t move0;     // first entry of its list of moves, for head 0 (each head has min(keep, len - keep) of them)
     int32_t first0;    // first entry of its counts of moves before each block, for head 0 (blocks + 1 each)
+    int64_t score0;    // first of its scores, [head][column][token] with tokens rounded up to 8; -1: more columns than have them kept
+    int64_t pad;
 };
-static_assert(sizeof(KvSeq) == 32, "KvSeq must stay 32 bytes");
+static_assert(sizeof(KvSeq) == 48, "KvSeq must stay 48 bytes");
 
 // work of one workgroup per head
 // work of one workgroup, for each head of the cache
@@ -59,6 +61,7 @@ struct KvAttend {
     float *part_o;  // sums of parts: [column][head][D]
     float *part_ml; // ... [column][head] {maximum, sum}
     float *stat;    // [row][query head] {maximum, 1 / sum}
+    float *scores;  // see KvSeq; NULL: not wanted
 };
 
 struct KvWeights {
@@ -107,7 +110,8 @@ struct slora_kv8_batch {
     uint64_t cuts_seen = 0;
     bool has_keep = false, short_rows = false, delivered = false;
     int32_t rows = 0, longest = 0, dest_blocks = 0;
-    int64_t part_cols = 0, moves = 0, firsts = 0; // scratch, per head of the cache
+    int32_t longest_few = 0, longest_many = 0; // of sequences of up to kKvFewCols columns, whose scores weights are taken from, and of others
+    int64_t part_cols = 0, moves = 0, firsts = 0, scores = 0; // scratch; part_cols for each head of the cache
 
     slora::Buffers *set = nullptr;
     slora::KvSeq *d_seqs = nullptr;

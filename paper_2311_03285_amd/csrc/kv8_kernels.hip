@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8.hpp"
 
@@ -34,6 +35,9 @@ __device__ __forceinline__ uint16_t narrow(float f)
     else
         return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
+
+// the wavefront's number in its workgroup, as a scalar: what follows from it takes no vector instructions
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave); }
 
 __device__ __forceinline__ float across_16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float across_32(float v) { return __shfl_xor(v, 32, kWave); }
@@ -96,7 +100,7 @@ template <int DT>
 __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAppend a)
 {
     const KvItem it = items[blockIdx.x / s.n_kv];
-    const int head = blockIdx.x % s.n_kv, which = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int head = blockIdx.x % s.n_kv, which = wave_number(), lane = threadIdx.x % kWave;
     const int64_t entry = table_entry(s, seqs[it.s].seq, it.a, head);
     uint8_t *page = s.pool + (int64_t)s.table[entry] * s.page_bytes;
     const int D = s.D, t0 = it.b, n = it.c;
@@ -291,7 +295,7 @@ __device__ __forceinline__ void load_pages(PartPages &pp, const KvShape &s, int 
 // A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
 // maxima, sums and O', and are put together in LDS at the end.
 template <int DT, int DB>
-__global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
+__global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
     constexpr int D = DB * 32, kWaves = kKvFewThreads / kWave;
     __shared__ PartPages pp;
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvIt
     const KvItem it = items[blockIdx.x / s.n_kv];
     const int head = blockIdx.x % s.n_kv;
     const KvSeq q = seqs[it.s];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
+    const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
     const int gpb = s.N / kKvGranule;
 
     // this lane's column, and how many tokens it sees
@@ -340,10 +344,9 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvIt
         for (int k = 0; k < DB; ++k) vr[k] = *reinterpret_cast<const u32x4 *>(pv + k * 256);
         e_next = pp.e[bv];
     };
-    int gr = g0 + wave * (kKvChunk / kKvGranule);
-    if (gr < g1) fetch(gr);
-    for (; gr < g1;) {
-        // operands of this chunk, then the next chunk's loads
+    constexpr int kStep = kWaves * (kKvChunk / kKvGranule);
+    auto work = [&](int gr, auto more) {
+        // operands of this chunk, then the next chunk's loads (not behind a branch: the compiler would wait for all loads where it joins)
         f32x4 sc[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -357,11 +360,23 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvIt
         const int ek = (int8_t)(e_next & 0xff), ev = e_next >> 8;
         const int token = (gr + g) * kKvGranule;
         const int bound = min(limit, g1 * kKvGranule) - token; // tokens of this lane's granule that its column sees
-        gr += kWaves * (kKvChunk / kKvGranule);
-        if (gr < g1) fetch(gr);
+        if constexpr (more.value) fetch(gr + kStep);
 
         const float f = unit * unit_of(ek), add = ev == kKvPoison ? __uint_as_float(0x7fc00000u) : (float)ev;
         float t[8], top = -INFINITY;
+        if (a.scores && q.score0 >= 0) {
+            float *at = a.scores + (q.score0 + ((int64_t)head * (q.rows * s.G) + col) * (int64_t)((q.len + 7) / 8 * 8)) + token;
+            f32x4 lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo[i] = i < bound ? sc[0][i] * f : -INFINITY;
+                hi[i] = i + 4 < bound ? sc[1][i] * f : -INFINITY;
+            }
+            if (real && token < q.len) {
+                *reinterpret_cast<f32x4 *>(at) = lo;
+                *reinterpret_cast<f32x4 *>(at + 4) = hi;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             t[i] = i < bound ? __builtin_fmaf(sc[i / 4][i % 4], f, add) : -INFINITY;
@@ -391,6 +406,12 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvIt
             o[2 * k] = mfma16(codes_to_f16x8(v[k].x, v[k].y), p, o[2 * k]);
             o[2 * k + 1] = mfma16(codes_to_f16x8(v[k].z, v[k].w), p, o[2 * k + 1]);
         }
+    };
+    int gr = g0 + wave * (kKvChunk / kKvGranule);
+    if (gr < g1) {
+        fetch(gr);
+        for (; gr + kStep < g1; gr += kStep) work(gr, std::true_type{});
+        work(gr, std::false_type{});
     }
     l += across_16(l);
     l += across_32(l);
@@ -446,46 +467,93 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_attend_few_kernel(const KvIt
     }
 }
 
-// Parts of a column put together, in the order of the sequence.  A workgroup = the columns of one tile, a wavefront one at a time.
+// Parts of a column put together: every wavefront takes some of them, in the order of the sequence, and the four are added in LDS.
 template <int DT, int DB>
 __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
-    constexpr int D = DB * 32, kPer = (D + kWave - 1) / kWave; // elements of a lane
+    constexpr int D = DB * 32, kPer = (D + kWave - 1) / kWave, kWaves = 4; // elements of a lane
+    __shared__ float merge[kWaves][kPer * kWave + 1];
     const KvItem it = items[blockIdx.x / s.n_kv];
-    const int head = blockIdx.x % s.n_kv;
+    const int head = blockIdx.x % s.n_kv, c = blockIdx.y;
+    if (c >= it.b) return;
     const KvSeq q = seqs[it.s];
-    const int lane = threadIdx.x % kWave;
-    for (int c = threadIdx.x / kWave; c < it.b; c += 256 / kWave) {
-        float top = -INFINITY;
-        for (int k = lane; k < it.c; k += kWave) top = fmaxf(top, a.part_ml[2 * ((int64_t)(it.poff + (int64_t)k * it.b + c) * s.n_kv + head)]);
+    const int wave = wave_number(), lane = threadIdx.x % kWave;
+    const int64_t first = (int64_t)(it.poff + c) * s.n_kv + head, step = (int64_t)it.b * s.n_kv;
+    float top = -INFINITY;
+    for (int k = lane; k < it.c; k += kWave) top = fmaxf(top, a.part_ml[2 * (first + k * step)]);
 #pragma unroll
-        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
-        const float use = top == -INFINITY ? 0.0f : top;
-        float total = 0.0f, sum[kPer] = {};
-        for (int k = 0; k < it.c; ++k) {
-            const int64_t at = (int64_t)(it.poff + (int64_t)k * it.b + c) * s.n_kv + head;
-            const float x = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use);
-            total = __builtin_fmaf(a.part_ml[2 * at + 1], x, total);
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
+    const float use = top == -INFINITY ? 0.0f : top;
+    float total = 0.0f, sum[kPer] = {};
+    constexpr int kAhead = 4;
+    for (int k0 = wave; k0 < it.c; k0 += kAhead * kWaves) {
+        float x[kAhead], l[kAhead], o[kAhead][kPer];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (lane + 64 * i < D) sum[i] = __builtin_fmaf(a.part_o[at * D + lane + 64 * i], x, sum[i]);
+        for (int j = 0; j < kAhead; ++j) {
+            const int k = k0 + j * kWaves;
+            const int64_t at = first + min(k, it.c - 1) * step;
+            x[j] = k < it.c ? __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use) : 0.0f;
+            l[j] = a.part_ml[2 * at + 1];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) o[j][i] = a.part_o[at * D + min(lane + 64 * i, D - 1)];
         }
-        const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
-        const float by = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (lane + 64 * i < D) a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + lane + 64 * i] = narrow<DT>(sum[i] * by);
-        if (lane == 0) {
-            float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
-            st[0] = use;
-            st[1] = by;
+        for (int j = 0; j < kAhead; ++j) {
+            if (k0 + j * kWaves >= it.c) break;
+            total = __builtin_fmaf(l[j], x[j], total);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) sum[i] = __builtin_fmaf(o[j][i], x[j], sum[i]);
         }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) merge[wave][lane + 64 * i] = sum[i];
+    if (lane == 0) merge[wave][kPer * kWave] = total;
+    __syncthreads();
+    total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += merge[w][kPer * kWave];
+    const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
+    const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
+    if ((int)threadIdx.x < D) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += merge[w][threadIdx.x];
+        a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + threadIdx.x] = narrow<DT>(v * by);
+    }
+    if (threadIdx.x == 0) {
+        float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
+        st[0] = use;
+        st[1] = by;
     }
 }
 
 // ---------------------------------------------------------------------------------------
 // what cached tokens draw
 // ---------------------------------------------------------------------------------------
+// ... from scores that attention left, of sequences with few columns: a thread per token.  Scores of tokens that a column does not see, and of
+// those behind the last that any sees, are not read.
+__global__ __launch_bounds__(256) void kv_weights_few_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvAttend a, KvWeights out)
+{
+    const KvSeq q = seqs[blockIdx.z];
+    const int head = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x, cols = q.rows * s.G;
+    if (t >= q.len || q.score0 < 0) return;
+    const int old = q.len - q.rows;
+    const int64_t stride = (q.len + 7) / 8 * 8;
+    const float *score = a.scores + q.score0 + (int64_t)head * cols * stride + t;
+    float v = 0.0f;
+    for (int c = 0; c < cols; ++c) {
+        const int row = c / s.G, h = head * s.G + c % s.G;
+        const float *st = a.stat + 2 * ((int64_t)(q.row0 + row) * s.n_kv * s.G + h);
+        if (!a.causal || t <= old + row) v = __builtin_fmaf(__builtin_amdgcn_exp2f(score[c * stride] - st[0]), st[1], v);
+    }
+    const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens + t;
+    if (t < old)
+        v += out.w_in[at];
+    else
+        out.pos[at] = q.seen - q.rows + t - old;
+    out.w_out[at] = v;
+}
+
 // The scores once more, 32 tokens a wavefront, with the maxima and sums that attention left; a lane adds up its tokens over its column of
 // every tile, then the 16 columns are added.
 template <int DT, int DB>
@@ -493,8 +561,9 @@ __global__ __launch_bounds__(kKvFewThreads) void kv_weights_kernel(const KvSeq *
 {
     constexpr int D = DB * 32, kWaves = kKvFewThreads / kWave;
     const KvSeq q = seqs[blockIdx.z];
+    if (q.score0 >= 0) return; // (kv_weights_few_kernel's)
     const int head = blockIdx.y;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
+    const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
     const int gr = (blockIdx.x * kWaves + wave) * (kKvChunk / kKvGranule), granules = (q.len + kKvGranule - 1) / kKvGranule;
     if (gr >= granules) return;
     const int gpb = s.N / kKvGranule, old = q.len - q.rows;
@@ -593,7 +662,7 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
 {
     constexpr int kTeams = Evict<W>::kTeams, kBits = Evict<W>::kBits, kBins = Evict<W>::kBins, kPer = Evict<W>::kPer;
     extern __shared__ uint32_t lds[];
-    const int team = threadIdx.x / kWave / W, wave = threadIdx.x / kWave % W, lane = threadIdx.x % kWave;
+    const int team = wave_number() / W, wave = wave_number() % W, lane = threadIdx.x % kWave;
     const int row = blockIdx.x * kTeams + team;
     if (row >= n_rows) return; // (a whole team; teams of one wavefront do not wait for each other)
     uint32_t *mine_lds = lds + team * (W * held + 2 * kBins + 4 * W);
@@ -932,7 +1001,7 @@ int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const K
                            (hipStream_t)stream, b->d_attend, b->d_seqs, shape, a);
         int32_t rc = check_launch("kv_attend");
         if (rc == SLORA_OK && !b->join.empty()) {
-            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv)), dim3(256), 0, (hipStream_t)stream,
+            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv), kKvFewCols), dim3(256), 0, (hipStream_t)stream,
                                b->d_join, b->d_seqs, shape, a);
             rc = check_launch("kv_join");
         }
@@ -943,8 +1012,14 @@ int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const K
 int32_t launch_kv_weights(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, const KvWeights &w, void *stream)
 {
     if (b->longest == 0) return SLORA_OK;
+    if (b->longest_few > 0) {
+        const dim3 grid((unsigned)((b->longest_few + 255) / 256), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
+        hipLaunchKernelGGL(kv_weights_few_kernel, grid, dim3(256), 0, (hipStream_t)stream, b->d_seqs, shape, a, w);
+        int32_t rc = check_launch("kv_weights_few");
+        if (rc != SLORA_OK || b->longest_many == 0) return rc;
+    }
     const int per = kKvFewThreads / kWave * kKvChunk;
-    const dim3 grid((unsigned)((b->longest + per - 1) / per), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
+    const dim3 grid((unsigned)((b->longest_many + per - 1) / per), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
     return by_shape(b->cache->pool->dtype, shape.D, [&](auto dt, auto db) {
         hipLaunchKernelGGL((kv_weights_kernel<dt.value, db.value>), grid, dim3(kKvFewThreads), 0, (hipStream_t)stream, b->d_seqs, shape, a, w);
         return check_launch("kv_weights");
