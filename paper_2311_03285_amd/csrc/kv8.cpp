@@ -180,7 +180,10 @@ void make_lists(slora_kv8_batch *b)
             for (int32_t k = 0; k < parts; ++k)
                 b->attend.push_back({(int32_t)i, (int32_t)c0, nc, k * step, std::min(granules, (k + 1) * step),
                                      parts > 1 ? (int32_t)(b->part_cols + (int64_t)k * nc) : -1, {0, 0}});
-            if (parts > 1) b->part_cols += (int64_t)parts * nc;
+            if (parts > 1) {
+                b->part_cols += (int64_t)parts * nc;
+                b->join_cols = std::max(b->join_cols, nc);
+            }
         }
     }
 }

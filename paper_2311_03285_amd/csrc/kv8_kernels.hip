@@ -259,13 +259,18 @@ __device__ __forceinline__ void load_q(const uint16_t *q, int g, f16x8 (&f)[DB],
 }
 
 // K of one token as first operands, from its row
-template <int DB>
+template <bool NT>
+__device__ __forceinline__ u32x4 load_once(const uint8_t *p)
+{
+    return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)) : *reinterpret_cast<const u32x4 *>(p);
+}
+template <int DB, bool NT = false>
 __device__ __forceinline__ void load_k(const uint8_t *row, int g, u32x4 (&raw)[(DB + 1) / 2])
 {
 #pragma unroll
     for (int p = 0; p < (DB + 1) / 2; ++p) {
         if (2 * p + 1 < DB) {
-            raw[p] = *reinterpret_cast<const u32x4 *>(row + 64 * p + 16 * g);
+            raw[p] = load_once<NT>(row + 64 * p + 16 * g);
         } else {
             const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 64 * p + 8 * g);
             raw[p] = u32x4{u.x, u.y, 0u, 0u};
@@ -338,10 +343,10 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         const int bk = (int)kv_div((uint32_t)gk, s.div_b), bv = (int)kv_div((uint32_t)gv, s.div_b);
         const uint8_t *pk = s.pool + (int64_t)pp.page[bk] * s.page_bytes + (int64_t)(gk - bk * gpb) * (2 * kKvGranule * D) + (n % 4) * D;
         const uint8_t *pv = s.pool + (int64_t)pp.page[bv] * s.page_bytes + (int64_t)(gv - bv * gpb) * (2 * kKvGranule * D) + kKvGranule * D + n * 16;
-        load_k<DB>(pk, g, kr[0]);
-        load_k<DB>(pk + 4 * D, g, kr[1]);
+        load_k<DB, true>(pk, g, kr[0]);
+        load_k<DB, true>(pk + 4 * D, g, kr[1]);
 #pragma unroll
-        for (int k = 0; k < DB; ++k) vr[k] = *reinterpret_cast<const u32x4 *>(pv + k * 256);
+        for (int k = 0; k < DB; ++k) vr[k] = load_once<true>(pv + k * 256);
         e_next = pp.e[bv];
     };
     constexpr int kStep = kWaves * (kKvChunk / kKvGranule);
@@ -1001,7 +1006,7 @@ int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const K
                            (hipStream_t)stream, b->d_attend, b->d_seqs, shape, a);
         int32_t rc = check_launch("kv_attend");
         if (rc == SLORA_OK && !b->join.empty()) {
-            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv), kKvFewCols), dim3(256), 0, (hipStream_t)stream,
+            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv), (unsigned)b->join_cols), dim3(256), 0, (hipStream_t)stream,
                                b->d_join, b->d_seqs, shape, a);
             rc = check_launch("kv_join");
         }
