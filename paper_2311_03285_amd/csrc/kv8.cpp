@@ -32,8 +32,11 @@ int32_t check_seqs(const slora_kv8 *cache, int32_t n, const int32_t *seqs)
     return SLORA_OK;
 }
 
-// Workgroups that a launch of attention is cut into, if the sequences are long enough: four or more for every compute unit.
-constexpr int64_t kPartTarget = 2048;
+// Workgroups that a launch of attention is cut into, if the sequences are long enough: twice three for every compute unit.  us a pass with 768, 1536, 2048,
+// 4096: 24 sequences of 200 - 1500 tokens 64.2 / 59.6 / 59.2 / 63.3, 64 of 500 - 8000 129 / 126 / 125 / 137, two of 90000 - 131000 86.8 / 84.9 / 91.0 / 108.
+constexpr int64_t kPartTarget = 1536;
+constexpr int64_t kManyTarget = 512;
+constexpr int32_t kManyLeast = 64;
 constexpr int32_t kPartLeast = 16; // granules: a chunk for each of the four wavefronts
 
 } // namespace
@@ -43,7 +46,7 @@ int32_t slora_kv8_batch::upload()
     slora_pool *pool = cache->pool;
     if (!pool->dev_base || seqs.empty()) return SLORA_OK;
     const size_t per = (size_t)cache->per_block();
-    const size_t items = append.size() + attend.size() + join.size();
+    const size_t items = append.size() + few.size() + many.size() + join.size();
     const size_t bytes = seqs.size() * sizeof(KvSeq) + items * sizeof(KvItem) + columns.size() * (1 + per) * sizeof(int32_t);
     int32_t rc = pool->take_set(&set, bytes, bytes);
     if (rc != SLORA_OK) return rc;
@@ -54,7 +57,8 @@ int32_t slora_kv8_batch::upload()
     };
     put(seqs);
     put(append);
-    put(attend);
+    put(few);
+    put(many);
     put(join);
     put(columns);
     for (int32_t c : columns) {
@@ -64,8 +68,9 @@ int32_t slora_kv8_batch::upload()
     }
     d_seqs = static_cast<KvSeq *>(set->d);
     d_append = reinterpret_cast<KvItem *>(d_seqs + seqs.size());
-    d_attend = d_append + append.size();
-    d_join = d_attend + attend.size();
+    d_few = d_append + append.size();
+    d_many = d_few + few.size();
+    d_join = d_many + many.size();
     d_columns = reinterpret_cast<int32_t *>(d_join + join.size());
     d_pages = d_columns + columns.size();
     void *up = nullptr;
@@ -156,10 +161,16 @@ void make_lists(slora_kv8_batch *b)
 {
     const slora_kv8 *c = b->cache;
     const int32_t G = c->n_heads / c->n_kv, gpb = c->N / kKvGranule;
-    int64_t work = 0;
-    for (const KvSeq &q : b->seqs) work += ((int64_t)q.rows * G + kKvFewCols - 1) / kKvFewCols * ((q.len + kKvGranule - 1) / kKvGranule) * c->n_kv;
-    int64_t part = std::max<int64_t>(kPartLeast, (work + kPartTarget - 1) / kPartTarget);
-    part = std::min<int64_t>(part, (int64_t)(kKvPartBlocks - 6) * gpb); // (whole chunks may add three granules, and begin inside a block)
+    // Sequences of few columns are cut into parts that make up kPartTarget workgroups, those of many columns (prompts), where a workgroup has
+    // more to do, kManyTarget.
+    auto is_many = [&](const KvSeq &q) { return (int64_t)q.rows * G >= kKvManyFrom; };
+    int64_t work[2] = {0, 0}; // granules times tiles of columns
+    for (const KvSeq &q : b->seqs) {
+        const int64_t cols = (int64_t)q.rows * G, each = is_many(q) ? kKvManyCols : kKvFewCols;
+        work[is_many(q)] += (cols + each - 1) / each * ((q.len + kKvGranule - 1) / kKvGranule) * c->n_kv;
+    }
+    int64_t part[2] = {std::max<int64_t>(kPartLeast, (work[0] + kPartTarget - 1) / kPartTarget), std::max<int64_t>(kManyLeast, (work[1] + kManyTarget - 1) / kManyTarget)};
+    for (int64_t &p : part) p = std::min<int64_t>(p, (int64_t)(kKvPartBlocks - 12) * gpb); // (whole chunks may add seven granules, and begin inside a block)
     for (size_t i = 0; i < b->seqs.size(); ++i) {
         const KvSeq &q = b->seqs[i];
         for (int32_t t = std::max(q.len - q.rows, 0); t < q.len;) {
@@ -169,23 +180,31 @@ void make_lists(slora_kv8_batch *b)
         }
         const int64_t cols = (int64_t)q.rows * G;
         const int32_t granules = (q.len + kKvGranule - 1) / kKvGranule;
-        for (int64_t c0 = 0; c0 < cols; c0 += kKvFewCols) {
-            const int32_t nc = (int32_t)std::min<int64_t>(kKvFewCols, cols - c0);
+        const bool many = is_many(q);
+        const int32_t each = many ? kKvManyCols : kKvFewCols, chunk = (many ? kKvManyTile : kKvChunk) / kKvGranule;
+        auto &list = many ? b->many : b->few;
+        for (int64_t c0 = 0; c0 < cols; c0 += each) {
+            const int32_t nc = (int32_t)std::min<int64_t>(each, cols - c0);
             // parts of whole chunks, all of about the same length
-            const int32_t n = (int32_t)std::max<int64_t>(1, (granules + part - 1) / part);
-            const int32_t chunk = kKvChunk / kKvGranule;
+            const int32_t n = (int32_t)std::max<int64_t>(1, (granules + part[many] - 1) / part[many]);
             const int32_t step = ((granules + n - 1) / n + chunk - 1) / chunk * chunk;
             const int32_t parts = step ? (granules + step - 1) / step : 1;
             if (parts > 1) b->join.push_back({(int32_t)i, (int32_t)c0, nc, parts, 0, (int32_t)b->part_cols, {0, 0}});
             for (int32_t k = 0; k < parts; ++k)
-                b->attend.push_back({(int32_t)i, (int32_t)c0, nc, k * step, std::min(granules, (k + 1) * step),
-                                     parts > 1 ? (int32_t)(b->part_cols + (int64_t)k * nc) : -1, {0, 0}});
+                list.push_back({(int32_t)i, (int32_t)c0, nc, k * step, std::min(granules, (k + 1) * step),
+                                parts > 1 ? (int32_t)(b->part_cols + (int64_t)k * nc) : -1, {0, 0}});
             if (parts > 1) {
                 b->part_cols += (int64_t)parts * nc;
                 b->join_cols = std::max(b->join_cols, nc);
             }
         }
     }
+    // the longest first; of equal ones those of later columns, which see more
+    auto granules_of = [&](const KvItem &x) {
+        const KvSeq &q = b->seqs[(size_t)x.s];
+        return std::min(x.d, (q.len - q.rows + (x.a + x.b - 1) / G + kKvGranule) / kKvGranule) - x.c;
+    };
+    std::stable_sort(b->many.begin(), b->many.end(), [&](const KvItem &x, const KvItem &y) { return granules_of(x) > granules_of(y); });
 }
 
 } // namespace
@@ -440,7 +459,7 @@ int32_t slora_kv8_batch_plan(slora_kv8 *c, slora_kv8_batch **out, int32_t n, con
     b->has_keep = keep != nullptr;
     b->cuts_seen = c->cuts;
     // (kernels count work by 32 bits)
-    const int64_t most = (int64_t)std::max({b->attend.size(), b->append.size(), b->join.size(), (size_t)1}) * c->n_kv;
+    const int64_t most = (int64_t)std::max({b->few.size(), b->many.size(), b->append.size(), b->join.size(), (size_t)1}) * c->n_kv;
     if (most >= int64_t(1) << 31 || b->part_cols * c->n_kv >= int64_t(1) << 31 || b->moves > INT32_MAX || b->firsts > INT32_MAX) {
         delete b;
         return fail(SLORA_ERANGE, "the batch is too large");

@@ -11,6 +11,9 @@ constexpr int kKvPoison = 127;       // exponent of a block that was given an in
 constexpr int kKvFewCols = 16;       // columns (rows x heads that share a head of the cache) of a tile of the matrix instruction
 constexpr int kKvFewThreads = 256;   // 4 wavefronts, which take turns at chunks of 32 tokens
 constexpr int kKvChunk = 32;
+constexpr int kKvManyTile = 64;      // tokens that a workgroup of prompts takes at a time
+constexpr int kKvManyCols = 128, kKvManyThreads = 256; // columns of a workgroup of prompts: 32 for each of four wavefronts
+constexpr int kKvManyFrom = 33;      // columns of a sequence from which it is one
 constexpr int kKvPartBlocks = 512;   // most blocks of a part of a sequence: their page numbers are held in LDS
 
 // a sequence of the batch
@@ -104,7 +107,7 @@ struct slora_kv8 {
 struct slora_kv8_batch {
     slora_kv8 *cache = nullptr;
     std::vector<slora::KvSeq> seqs;
-    std::vector<slora::KvItem> append, attend, join;
+    std::vector<slora::KvItem> append, few, many, join;
     std::vector<int32_t> cuts; // of each sequence when the batch was planned
     std::vector<int32_t> columns; // sequence * max_blocks + block: pages that the first call brings into the table
     uint64_t cuts_seen = 0;
@@ -115,7 +118,7 @@ struct slora_kv8_batch {
 
     slora::Buffers *set = nullptr;
     slora::KvSeq *d_seqs = nullptr;
-    slora::KvItem *d_append = nullptr, *d_attend = nullptr, *d_join = nullptr;
+    slora::KvItem *d_append = nullptr, *d_few = nullptr, *d_many = nullptr, *d_join = nullptr;
     int32_t *d_columns = nullptr, *d_pages = nullptr;
     void *last_stream = nullptr;
     bool order_recorded = false;

@@ -226,36 +226,47 @@ __device__ __forceinline__ int element_of(int j, int g)
     return j / 2 * 2 + 1 < DB ? j / 2 * 64 + 16 * g + 8 * (j % 2) : j * 32 + 8 * g;
 }
 
-// q of one column as second operands, and the power of two to multiply its scores by
-template <int DT, int DB>
-__device__ __forceinline__ void load_q(const uint16_t *q, int g, f16x8 (&f)[DB], float &unit)
+// q of one column as second operands, element(j) on for step j, and the power of two to multiply its scores by.  Lanes that differ in the bits
+// of LANES hold other elements of the same column.
+template <int DT, int STEPS, int LANES, typename F>
+__device__ __forceinline__ void load_column(const uint16_t *q, F element, f16x8 (&f)[STEPS], float &unit)
 {
     unit = 1.0f;
     if constexpr (DT == SLORA_F16) {
 #pragma unroll
-        for (int j = 0; j < DB; ++j)
-            f[j] = q ? __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(q + element_of<DB>(j, g))) : f16x8{};
+        for (int j = 0; j < STEPS; ++j) f[j] = q ? __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(q + element(j))) : f16x8{};
     } else {
-        u32x4 raw[DB];
+        u32x4 raw[STEPS];
         uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < DB; ++j) {
-            raw[j] = q ? *reinterpret_cast<const u32x4 *>(q + element_of<DB>(j, g)) : u32x4{0u, 0u, 0u, 0u};
+        for (int j = 0; j < STEPS; ++j) {
+            raw[j] = q ? *reinterpret_cast<const u32x4 *>(q + element(j)) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
             for (int k = 0; k < 4; ++k) top = max(top, max(raw[j][k] & 0x7fffu, (raw[j][k] >> 16) & 0x7fffu));
         }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16, kWave));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
+#pragma unroll
+        for (int x = 16; x < kWave; x *= 2)
+            if (LANES & x) top = max(top, (uint32_t)__shfl_xor((int)top, x, kWave));
         // largest magnitude 2^(x - 127) .. : times 2^(141 - x) it lies in [2^14, 2^15); both powers are kept normal numbers
         const int x = (int)(top >> 7);
         const int up = x == 0 || x == 255 ? 0 : min(max(141 - x, -100), 100);
         const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
         unit = __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
-        for (int j = 0; j < DB; ++j)
+        for (int j = 0; j < STEPS; ++j)
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[j][k] = (_Float16)(__uint_as_float((raw[j][k / 2] >> (16 * (k % 2))) << 16) * scale);
     }
+}
+template <int DT, int DB>
+__device__ __forceinline__ void load_q(const uint16_t *q, int g, f16x8 (&f)[DB], float &unit)
+{
+    load_column<DT, DB, 48>(q, [=](int j) { return element_of<DB>(j, g); }, f, unit);
+}
+template <int DT, int DB>
+__device__ __forceinline__ void load_q32(const uint16_t *q, int h, f16x8 (&f)[2 * DB], float &unit)
+{
+    load_column<DT, 2 * DB, 32>(q, [=](int j) { return 16 * j + 8 * h; }, f, unit);
 }
 
 // K of one token as first operands, from its row
@@ -469,6 +480,217 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
                 st[1] = by;
             }
         }
+    }
+}
+
+// Many columns (prompts).  Matrix instruction 32 x 32 x 16: lane l = 32 h + n supplies k-values 8 h .. 8 h + 7 of row or column n and receives
+// rows 8 b + 4 h + i of column n (register 4 b + i).
+//
+// A workgroup = an item of up to 128 columns, 32 to a wavefront, that walk the tokens in tiles of 64 together.  A tile's codes are turned into
+// binary16 once, on the way into LDS: K in units of 8 elements of a token, [unit][token] (tokens 8 apart change places in every
+// other pair of units, for the sake of the writes), V in units of 8 tokens of an element as its granules hold them - so that every
+// operand is one read of 16 bytes, lane by lane in order.  While one tile is worked on, the next one's loads are under way; it
+// goes into the other buffer afterwards, and one barrier ends the round.
+//
+// As above the scores are transposed, and which token is which row is chosen so that a lane's scores are the k-values that it
+// has to supply next: row 16 s + 8 b + 4 h + i of a half of the tile is its token 16 s + 8 h + 4 b + i, of granule 2 s + h.
+// The maximum is only raised when a score exceeds it by 2^kSlack: until then probabilities stay below 2^kSlack, which costs them nothing.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+constexpr int kManyTile = kKvManyTile, kManyGranules = kManyTile / kKvGranule;
+constexpr float kSlack = 8.0f;
+
+template <int DB>
+struct ManyLds {
+    static constexpr int kUnits = kManyTile * DB * 4; // of 16 bytes, K's or V's of a tile
+    u32x4 k[2][kUnits], v[2][kUnits];
+    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, ev, 2^-ev of each granule
+    PartPages pages;
+};
+
+template <int DT, int DB>
+__global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_many_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
+{
+    constexpr int D = DB * 32, kSteps = 2 * DB;
+    extern __shared__ u32x4 lds_bytes[];
+    ManyLds<DB> &lds = *reinterpret_cast<ManyLds<DB> *>(lds_bytes);
+    const KvItem it = items[blockIdx.x / s.n_kv];
+    const int head = blockIdx.x % s.n_kv;
+    const KvSeq q = seqs[it.s];
+    const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 32, h = lane / 32;
+    const int gpb = s.N / kKvGranule, old = q.len - q.rows;
+
+    const int col = it.a + wave * 32 + n, row = col / s.G;
+    const bool real = wave * 32 + n < it.b;
+    const int last_row = (it.a + it.b - 1) / s.G;
+    const int limit = !real ? q.len : a.causal ? min(old + row + 1, q.len) : q.len; // tokens that this lane's column sees
+    const int tokens = a.causal ? min(old + last_row + 1, q.len) : q.len;
+    const int g0 = it.c, g1 = min(it.d, (max(tokens, 0) + kKvGranule - 1) / kKvGranule);
+    // of this wavefront's columns: what all of them see, what any sees
+    const int all_see = a.causal ? min(old + (it.a + min(wave * 32, it.b - 1)) / s.G + 1, q.len) : q.len;
+    const int any_sees = wave * 32 >= it.b ? 0 : a.causal ? min(old + (it.a + min(wave * 32 + 31, it.b - 1)) / s.G + 1, q.len) : q.len;
+    const int block0 = g0 / gpb, base = block0 * gpb;
+    if (g1 > g0) load_pages(lds.pages, s, q.seq, head, block0, (g1 - 1) / gpb + 1 - block0);
+
+    f16x8 qf[kSteps];
+    float unit;
+    const int qhead = head * s.G + col % s.G;
+    load_q32<DT, DB>(real ? a.q + (int64_t)(q.row0 + row) * a.q_stride + (int64_t)qhead * D : nullptr, h, qf, unit);
+    unit *= a.scale;
+    __syncthreads();
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int k = 0; k < DB; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[k][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    // a tile's pieces of 16 bytes, D to a granule (K's first), 256 at a time
+    u32x4 raw[DB];
+    auto fetch = [&](int g) {
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            const int u = threadIdx.x + i * kKvManyThreads, gk = min(g + u / D, g1 - 1) - base;
+            const int b = (int)kv_div((uint32_t)gk, s.div_b);
+            raw[i] = *reinterpret_cast<const u32x4 *>(s.pool + (int64_t)lds.pages.page[b] * s.page_bytes + (int64_t)(gk - b * gpb) * (2 * kKvGranule * D) + u % D * 16);
+        }
+    };
+    auto put = [&](int buffer, int g) {
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            const int u = threadIdx.x + i * kKvManyThreads, w = u % D;
+            const u32x4 lo = __builtin_bit_cast(u32x4, codes_to_f16x8(raw[i].x, raw[i].y)), hi = __builtin_bit_cast(u32x4, codes_to_f16x8(raw[i].z, raw[i].w));
+            if (w < D / 2) { // 16 elements of a token: units 2 c, 2 c + 1
+                const int token = u / D * kKvGranule + w / (D / 16), c = w % (D / 16), at = token ^ (c % 2 * 8);
+                lds.k[buffer][2 * c * kManyTile + at] = lo;
+                lds.k[buffer][(2 * c + 1) * kManyTile + at] = hi;
+            } else { // two elements' eight tokens
+                const int at = u / D * D + 2 * (w - D / 2);
+                lds.v[buffer][at] = lo;
+                lds.v[buffer][at + 1] = hi;
+            }
+        }
+        if (threadIdx.x < kManyGranules) {
+            const int gk = min(g + (int)threadIdx.x, g1 - 1) - base, e = lds.pages.e[kv_div((uint32_t)gk, s.div_b)];
+            const int ek = (int8_t)(e & 0xff), ev = e >> 8;
+            lds.unit[buffer][threadIdx.x] = unit_of(ek);
+            lds.add[buffer][threadIdx.x] = ev == kKvPoison ? __uint_as_float(0x7fc00000u) : (float)ev;
+            lds.less[buffer][threadIdx.x] = unit_of(-ev);
+        }
+    };
+    // this lane's token in row n of a half of the tile, and its place in LDS for units 2 s + h, s even and odd
+    const int token_n = n / 16 * 16 + n / 4 % 2 * 8 + n / 8 % 2 * 4 + n % 4;
+    if (g1 > g0) {
+        fetch(g0);
+        put(0, g0);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int g = g0; g < g1; g += kManyGranules, buffer ^= 1) {
+        const bool more = g + kManyGranules < g1;
+        if (more) fetch(g + kManyGranules);
+        const int first = g * kKvGranule;
+        if (first < any_sees) {
+            f32x16 sc[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) { // unit 2 j + h: c = j
+                    const f16x8 kf = __builtin_bit_cast(f16x8, lds.k[buffer][(2 * j + h) * kManyTile + ((t * 32 + token_n) ^ (j % 2 * 8))]);
+                    sc[t] = mfma32(kf, qf[j], sc[t]);
+                }
+            }
+            // registers 8 s .. 8 s + 7 of half t: granule 4 t + 2 s + h
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float f = unit * lds.unit[buffer][4 * t + 2 * r + h], add = lds.add[buffer][4 * t + 2 * r + h];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sc[t][8 * r + i] = __builtin_fmaf(sc[t][8 * r + i], f, add);
+                }
+            if (first + kManyTile > min(all_see, g1 * kKvGranule)) {
+                const int bound = min(limit, g1 * kKvGranule) - first - 8 * h;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * 32 + i / 8 * 16 + i % 8 >= bound) sc[t][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
+            top = fmaxf(top, across_32(top));
+            if (__any(top > m + kSlack || (m == -INFINITY && top > m))) {
+                const float m_new = fmaxf(m, top), keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= keep;
+#pragma unroll
+                for (int k = 0; k < DB; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[k][i] *= keep;
+            }
+            const float use = m == -INFINITY ? 0.0f : m;
+            f16x8 p[2][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = __builtin_amdgcn_exp2f(sc[t][8 * r + i] - use);
+                        sum += x;
+                        p[t][r][i] = (_Float16)x;
+                    }
+                    l = __builtin_fmaf(sum, lds.less[buffer][4 * t + 2 * r + h], l);
+                }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int k = 0; k < DB; ++k)
+                        o[k] = mfma32(__builtin_bit_cast(f16x8, lds.v[buffer][(4 * t + 2 * r + h) * D + 32 * k + n]), p[t][r], o[k]);
+        }
+        if (more) put(buffer ^ 1, g + kManyGranules);
+        __syncthreads();
+    }
+    l += across_32(l);
+    if (!real) return;
+    // elements 32 k + 8 b + 4 h + i of column n are register 4 b + i of o[k]
+    if (it.poff >= 0) {
+        const int64_t at = (int64_t)(it.poff + wave * 32 + n) * s.n_kv + head;
+#pragma unroll
+        for (int k = 0; k < DB; ++k)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<f32x4 *>(a.part_o + at * D + 32 * k + 8 * b + 4 * h) = f32x4{o[k][4 * b], o[k][4 * b + 1], o[k][4 * b + 2], o[k][4 * b + 3]};
+        if (h == 0) {
+            a.part_ml[2 * at] = m;
+            a.part_ml[2 * at + 1] = l;
+        }
+        return;
+    }
+    const float by = l == 0.0f ? 0.0f : 1.0f / l; // a row that sees nothing is 0
+    uint16_t *out = a.out + (int64_t)(q.row0 + row) * a.out_stride + (int64_t)qhead * D;
+#pragma unroll
+    for (int k = 0; k < DB; ++k)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            *reinterpret_cast<u32x2 *>(out + 32 * k + 8 * b + 4 * h) =
+                u32x2{(uint32_t)narrow<DT>(o[k][4 * b] * by) | (uint32_t)narrow<DT>(o[k][4 * b + 1] * by) << 16,
+                      (uint32_t)narrow<DT>(o[k][4 * b + 2] * by) | (uint32_t)narrow<DT>(o[k][4 * b + 3] * by) << 16};
+    if (h == 0) {
+        float *st = a.stat + 2 * ((int64_t)(q.row0 + row) * s.n_kv * s.G + qhead);
+        st[0] = m == -INFINITY ? 0.0f : m;
+        st[1] = by;
     }
 }
 
@@ -1001,10 +1223,21 @@ int32_t launch_kv_append(const slora_kv8_batch *b, const KvShape &shape, const K
 
 int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, void *stream)
 {
+    hipStream_t st = (hipStream_t)stream;
     return by_shape(b->cache->pool->dtype, shape.D, [&](auto dt, auto db) {
-        hipLaunchKernelGGL((kv_attend_few_kernel<dt.value, db.value>), dim3((unsigned)(b->attend.size() * shape.n_kv)), dim3(kKvFewThreads), 0,
-                           (hipStream_t)stream, b->d_attend, b->d_seqs, shape, a);
-        int32_t rc = check_launch("kv_attend");
+        int32_t rc = SLORA_OK;
+        if (!b->many.empty()) { // (the longer ones)
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_attend_many_kernel<dt.value, db.value>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+            if (e != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
+            hipLaunchKernelGGL((kv_attend_many_kernel<dt.value, db.value>), dim3((unsigned)(b->many.size() * shape.n_kv)), dim3(kKvManyThreads),
+                               sizeof(ManyLds<db.value>), st, b->d_many, b->d_seqs, shape, a);
+            rc = check_launch("kv_attend_many");
+        }
+        if (rc == SLORA_OK && !b->few.empty()) {
+            hipLaunchKernelGGL((kv_attend_few_kernel<dt.value, db.value>), dim3((unsigned)(b->few.size() * shape.n_kv)), dim3(kKvFewThreads), 0, st, b->d_few,
+                               b->d_seqs, shape, a);
+            rc = check_launch("kv_attend_few");
+        }
         if (rc == SLORA_OK && !b->join.empty()) {
             hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv), (unsigned)b->join_cols), dim3(256), 0, (hipStream_t)stream,
                                b->d_join, b->d_seqs, shape, a);
