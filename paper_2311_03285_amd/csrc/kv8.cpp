@@ -35,6 +35,8 @@ int32_t check_seqs(const slora_kv8 *cache, int32_t n, const int32_t *seqs)
 // Workgroups that a launch of attention is cut into, if the sequences are long enough: twice three for every compute unit.  us a pass with 768, 1536, 2048,
 // 4096: 24 sequences of 200 - 1500 tokens 64.2 / 59.6 / 59.2 / 63.3, 64 of 500 - 8000 129 / 126 / 125 / 137, two of 90000 - 131000 86.8 / 84.9 / 91.0 / 108.
 constexpr int64_t kPartTarget = 1536;
+// Prompts, two workgroups of which fit a compute unit: us a pass with 256, 512, 1024 workgroups: a chunk of 512 behind 30000 983 / 741 / 743, eight of 64 behind
+// 4000 147 / 134 / 151, one of 2048 98 / 98 / 118; parts of at least 128, 256, 512 tokens, a prompt of 512: 37.5 / 35.7 / 33.8.
 constexpr int64_t kManyTarget = 512;
 constexpr int32_t kManyLeast = 64;
 constexpr int32_t kPartLeast = 16; // granules: a chunk for each of the four wavefronts
@@ -196,6 +198,7 @@ void make_lists(slora_kv8_batch *b)
             if (parts > 1) {
                 b->part_cols += (int64_t)parts * nc;
                 b->join_cols = std::max(b->join_cols, nc);
+                b->join_parts = std::max(b->join_parts, parts);
             }
         }
     }

@@ -694,17 +694,18 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     }
 }
 
-// Parts of a column put together: every wavefront takes some of them, in the order of the sequence, and the four are added in LDS.
-template <int DT, int DB>
+// Parts of a column put together, in the order of the sequence.  W = 4: a workgroup per column, whose wavefronts take parts in turn and are
+// added in LDS; W = 1, where there are few parts: a wavefront per column.
+template <int DT, int DB, int W>
 __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
-    constexpr int D = DB * 32, kPer = (D + kWave - 1) / kWave, kWaves = 4; // elements of a lane
-    __shared__ float merge[kWaves][kPer * kWave + 1];
+    constexpr int D = DB * 32, kPer = (D + kWave - 1) / kWave; // elements of a lane
+    __shared__ float merge[W][kPer * kWave + 1];
     const KvItem it = items[blockIdx.x / s.n_kv];
-    const int head = blockIdx.x % s.n_kv, c = blockIdx.y;
+    const int head = blockIdx.x % s.n_kv, wave = wave_number() % W, lane = threadIdx.x % kWave;
+    const int c = (int)blockIdx.y * (4 / W) + wave_number() / W;
     if (c >= it.b) return;
     const KvSeq q = seqs[it.s];
-    const int wave = wave_number(), lane = threadIdx.x % kWave;
     const int64_t first = (int64_t)(it.poff + c) * s.n_kv + head, step = (int64_t)it.b * s.n_kv;
     float top = -INFINITY;
     for (int k = lane; k < it.c; k += kWave) top = fmaxf(top, a.part_ml[2 * (first + k * step)]);
@@ -713,11 +714,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__
     const float use = top == -INFINITY ? 0.0f : top;
     float total = 0.0f, sum[kPer] = {};
     constexpr int kAhead = 4;
-    for (int k0 = wave; k0 < it.c; k0 += kAhead * kWaves) {
+    for (int k0 = wave; k0 < it.c; k0 += kAhead * W) {
         float x[kAhead], l[kAhead], o[kAhead][kPer];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int k = k0 + j * kWaves;
+            const int k = k0 + j * W;
             const int64_t at = first + min(k, it.c - 1) * step;
             x[j] = k < it.c ? __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use) : 0.0f;
             l[j] = a.part_ml[2 * at + 1];
@@ -726,28 +727,31 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (k0 + j * kWaves >= it.c) break;
+            if (k0 + j * W >= it.c) break;
             total = __builtin_fmaf(l[j], x[j], total);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) sum[i] = __builtin_fmaf(o[j][i], x[j], sum[i]);
         }
     }
+    if constexpr (W > 1) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) merge[wave][lane + 64 * i] = sum[i];
-    if (lane == 0) merge[wave][kPer * kWave] = total;
-    __syncthreads();
-    total = 0.0f;
+        for (int i = 0; i < kPer; ++i) merge[wave][lane + 64 * i] = sum[i];
+        if (lane == 0) merge[wave][kPer * kWave] = total;
+        __syncthreads();
+        if (wave > 0) return;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += merge[w][kPer * kWave];
+        for (int w = 1; w < W; ++w) {
+            total += merge[w][kPer * kWave];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) sum[i] += merge[w][lane + 64 * i];
+        }
+    }
     const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
     const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
-    if ((int)threadIdx.x < D) {
-        float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += merge[w][threadIdx.x];
-        a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + threadIdx.x] = narrow<DT>(v * by);
-    }
-    if (threadIdx.x == 0) {
+    for (int i = 0; i < kPer; ++i)
+        if (lane + 64 * i < D) a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + lane + 64 * i] = narrow<DT>(sum[i] * by);
+    if (lane == 0) {
         float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
         st[0] = use;
         st[1] = by;
@@ -1221,6 +1225,8 @@ int32_t launch_kv_append(const slora_kv8_batch *b, const KvShape &shape, const K
     return check_launch("kv_append");
 }
 
+constexpr int32_t kFewParts = 16; // of a column, up to which a wavefront puts them together alone
+
 int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, void *stream)
 {
     hipStream_t st = (hipStream_t)stream;
@@ -1239,8 +1245,12 @@ int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const K
             rc = check_launch("kv_attend_few");
         }
         if (rc == SLORA_OK && !b->join.empty()) {
-            hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value>), dim3((unsigned)(b->join.size() * shape.n_kv), (unsigned)b->join_cols), dim3(256), 0, (hipStream_t)stream,
-                               b->d_join, b->d_seqs, shape, a);
+            const unsigned items = (unsigned)(b->join.size() * shape.n_kv);
+            if (b->join_parts > kFewParts)
+                hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value, 4>), dim3(items, (unsigned)b->join_cols), dim3(256), 0, st, b->d_join, b->d_seqs, shape, a);
+            else
+                hipLaunchKernelGGL((kv_join_kernel<dt.value, db.value, 1>), dim3(items, (unsigned)(b->join_cols + 3) / 4), dim3(256), 0, st, b->d_join, b->d_seqs,
+                                   shape, a);
             rc = check_launch("kv_join");
         }
         return rc;
