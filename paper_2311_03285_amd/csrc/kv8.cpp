@@ -437,6 +437,7 @@ int32_t slora_kv8_batch_plan(slora_kv8 *c, slora_kv8_batch **out, int32_t n, con
             }
             s.move0 = (int32_t)b->moves;
             s.first0 = (int32_t)b->firsts;
+            b->most_going = std::max(b->most_going, s.len - s.keep);
             if (s.keep < s.len) {
                 b->moves += (int64_t)std::min(s.keep, s.len - s.keep) * c->n_kv;
                 b->firsts += (int64_t)(c->blocks(s.keep) + 1) * c->n_kv;

@@ -113,6 +113,7 @@ struct slora_kv8_batch {
     uint64_t cuts_seen = 0;
     bool has_keep = false, short_rows = false, delivered = false;
     int32_t rows = 0, longest = 0, dest_blocks = 0, join_cols = 0, join_parts = 0; // (the last two: most of a join item)
+    int32_t most_going = 0; // most tokens that an eviction drops from a sequence
     int32_t longest_few = 0, longest_many = 0; // of sequences of up to kKvFewCols columns, whose scores weights are taken from, and of others
     int64_t part_cols = 0, moves = 0, firsts = 0, scores = 0; // scratch; part_cols for each head of the cache
 

@@ -112,10 +112,15 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
     const int per_row = D / 8, rows_at_once = kWave / per_row, r0 = lane / per_row, c0 = lane % per_row * 8;
     const bool on = r0 < rows_at_once;
     uint32_t top = 0; // largest magnitude, as the bits of its 16-bit form (which order as the values do)
-    for (int r = r0; on && r < n; r += rows_at_once) {
-        const u32x4 u = *reinterpret_cast<const u32x4 *>(x + r * stride + c0);
+    constexpr int kAhead = 4; // rows of a lane that are loaded together (those behind the last: the last once more)
+    u32x4 kept[kAhead] = {}; // ... of which a single round's stay for K's second pass
+    for (int r = r0; on && r < n; r += kAhead * rows_at_once) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top = max(top, max(u[k] & 0x7fffu, (u[k] >> 16) & 0x7fffu));
+        for (int j = 0; j < kAhead; ++j) kept[j] = *reinterpret_cast<const u32x4 *>(x + min(r + j * rows_at_once, n - 1) * stride + c0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, max(kept[j][k] & 0x7fffu, (kept[j][k] >> 16) & 0x7fffu));
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, kWave));
@@ -136,15 +141,20 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
                 u.y = shift_codes(u.y, factor);
                 *p = u;
             }
-        for (int r = r0; on && r < n; r += rows_at_once) {
-            const u32x4 u = *reinterpret_cast<const u32x4 *>(x + r * stride + c0);
-            uint32_t o[2] = {0, 0};
+        for (int r = r0; on && r < n; r += kAhead * rows_at_once) {
+            if (n > kAhead * rows_at_once)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float v = widen<DT>((uint16_t)(u[k / 2] >> (16 * (k % 2))));
-                if (!poison) o[k / 4] |= ((uint32_t)code_of(v, inverse) & 0xffu) << (8 * (k % 4));
+                for (int j = 0; j < kAhead; ++j) kept[j] = *reinterpret_cast<const u32x4 *>(x + min(r + j * rows_at_once, n - 1) * stride + c0);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                uint32_t o[2] = {0, 0};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float v = widen<DT>((uint16_t)(kept[j][k / 2] >> (16 * (k % 2))));
+                    if (!poison) o[k / 4] |= ((uint32_t)code_of(v, inverse) & 0xffu) << (8 * (k % 4));
+                }
+                if (r + j * rows_at_once < n) *reinterpret_cast<u32x2 *>(row_at(t0 + r + j * rows_at_once) + c0) = u32x2{o[0], o[1]};
             }
-            *reinterpret_cast<u32x2 *>(row_at(t0 + r) + c0) = u32x2{o[0], o[1]};
         }
     } else {
         const int first = grown ? 0 : t0 / kKvGranule, last = (t0 + n - 1) / kKvGranule;
@@ -166,7 +176,7 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
             }
             uint32_t raw[kKvGranule];
 #pragma unroll
-            for (int t = 0; t < kKvGranule; ++t) raw[t] = t >= from && t < to ? *reinterpret_cast<const uint32_t *>(x + (lo + t - t0) * stride + d) : 0;
+            for (int t = 0; t < kKvGranule; ++t) raw[t] = *reinterpret_cast<const uint32_t *>(x + min(max(lo + t - t0, 0), n - 1) * stride + d);
 #pragma unroll
             for (int t = 0; t < kKvGranule; ++t) {
                 if (t < from || t >= to) continue;
@@ -1085,6 +1095,152 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
     }
 }
 
+// A cache at its budget, which has few tokens more than it keeps after each step: a wavefront per row, in one launch.  The token that goes is the one of
+// least rank, of equal ones that in the highest slot; the next one is the least behind it in this order.  What stays of
+// the slots behind the budget moves at once.
+constexpr int kEvictFew = 4, kEvictFewTokens = 8192;
+__global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restrict__ seqs, int n_rows, KvShape s, KvEvict e)
+{
+    const int row = blockIdx.x * 4 + wave_number(), lane = threadIdx.x % kWave, D = s.D;
+    if (row >= n_rows) return;
+    const KvSeq q = seqs[row / s.n_kv];
+    const int head = row % s.n_kv;
+    const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens;
+    const float *w = e.w_in + at;
+    const int32_t *pos = e.pos_in + at;
+    float *const w_out = e.w_out + at;
+    int32_t *const pos_out = e.pos_out + at;
+    const bool copies = e.w_out != e.w_in || e.pos_out != e.pos_in;
+    const int going = q.keep == 0 ? 0 : q.len - q.keep; // (of none that stay nothing is written)
+    if (q.keep == 0 && q.len > 0) return;
+    const int recent_from = q.seen - min(min(e.recent, q.keep), q.seen);
+    int gone[kEvictFew]; // slots, in the order found
+    uint32_t last_rank = 0;
+    int last_slot = INT32_MAX;
+    for (int turn = 0; turn < max(going, 1); ++turn) {
+        uint32_t least = 0xffffffffu;
+        int slot = -1;
+        constexpr int kAhead = 8;
+        for (uint32_t j = 0; j < (uint32_t)q.len; j += kAhead * kWave) {
+            float a[kAhead];
+            int32_t p[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const uint32_t i = min(j + k * kWave + lane, (uint32_t)q.len - 1);
+                a[k] = w[i];
+                p[k] = pos[i];
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const uint32_t i = j + k * kWave + lane;
+                if (turn == 0 && copies && i < (uint32_t)q.keep) { // (places that fall free are written again, by what moves there)
+                    w_out[i] = a[k];
+                    pos_out[i] = p[k];
+                }
+                const uint32_t r = rank_of(a[k], p[k], recent_from);
+                const bool behind = r > last_rank || (r == last_rank && (int)i < last_slot);
+                if (i < (uint32_t)q.len && behind && r <= least) { // (later slots of an equal rank take the place of earlier ones)
+                    least = r;
+                    slot = (int)i;
+                }
+            }
+        }
+        if (going == 0) return;
+#pragma unroll
+        for (int x = 32; x; x >>= 1) {
+            const uint32_t r = (uint32_t)__shfl_xor((int)least, x, kWave);
+            const int i = __shfl_xor(slot, x, kWave);
+            if (i >= 0 && (slot < 0 || r < least || (r == least && i > slot))) least = r, slot = i;
+        }
+        slot = __builtin_amdgcn_readfirstlane(slot);
+        last_rank = (uint32_t)__builtin_amdgcn_readfirstlane((int)least);
+        last_slot = slot;
+#pragma unroll
+        for (int k = 0; k < kEvictFew; ++k)
+            if (k == turn) gone[k] = slot;
+    }
+    // places and moves, both in the order of the slots: lane k has the k-th slot behind the budget, and the k-th that goes
+    __shared__ int moves[4][kEvictFew][2];
+    auto &move = moves[wave_number()];
+    int mine = INT32_MAX;
+#pragma unroll
+    for (int k = 0; k < kEvictFew; ++k)
+        if (k == lane && k < going) mine = gone[k];
+    bool stays = lane < going;
+#pragma unroll
+    for (int k = 0; k < kEvictFew; ++k) stays = stays && !(k < going && gone[k] == q.keep + lane);
+    const uint64_t staying = __ballot(stays);
+    int place = 0;
+#pragma unroll
+    for (int k = 0; k < kEvictFew; ++k) place += k < going && gone[k] < mine;
+    const int n = (int)__popcll(staying); // as many places are before the budget
+    if (stays) move[__popcll(staying & ((uint64_t(1) << lane) - 1))][0] = q.keep + lane;
+    if (mine < q.keep) move[place][1] = mine;
+    team_sync<1>();
+    if (lane < n) {
+        w_out[move[lane][1]] = w[move[lane][0]];
+        pos_out[move[lane][1]] = pos[move[lane][0]];
+    }
+    const int granule_bytes = 2 * kKvGranule * D;
+    auto granule = [&](int64_t entry, int t) { return s.pool + (int64_t)s.table[entry] * s.page_bytes + (int64_t)(t / kKvGranule) * granule_bytes; };
+    // a block at a time: all of its moves, since its exponent is that of all
+    for (int m0 = 0, m1; m0 < n; m0 = m1) {
+        const int block = move[m0][1] / s.N;
+        const int64_t entry = table_entry(s, q.seq, block, head);
+        const int was_k = s.exps[2 * entry], was_v = s.exps[2 * entry + 1];
+        int now_k = was_k, now_v = was_v;
+        for (m1 = m0; m1 < n && move[m1][1] / s.N == block; ++m1) {
+            const int64_t from = table_entry(s, q.seq, move[m1][0] / s.N, head);
+            now_k = max(now_k, (int)s.exps[2 * from]);
+            now_v = max(now_v, (int)s.exps[2 * from + 1]);
+        }
+        const int last = min(s.N, q.keep - block * s.N); // slots of the block that stay in use
+        // exponents of sources as they are before this block's change (a block about the budget has places and sources)
+        uint32_t k4[kEvictFew];
+        uint8_t v1[kEvictFew][4];
+        float fk[kEvictFew], fv[kEvictFew];
+#pragma unroll
+        for (int k = 0; k < kEvictFew; ++k) {
+            if (m0 + k >= m1) break;
+            const int from = move[m0 + k][0], t = from % s.N;
+            const int64_t e0 = table_entry(s, q.seq, from / s.N, head);
+            fk[k] = shift_factor(s.exps[2 * e0], now_k);
+            fv[k] = shift_factor(s.exps[2 * e0 + 1], now_v);
+            const uint8_t *g = granule(e0, t);
+            if (lane < D / 4) k4[k] = *(reinterpret_cast<const uint32_t *>(g + t % kKvGranule * D) + lane);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (lane + x * kWave < D) v1[k][x] = g[kKvGranule * D + (lane + x * kWave) * kKvGranule + t % kKvGranule];
+        }
+        if (now_k != was_k || now_v != was_v) {
+            const float grow_k = shift_factor(was_k, now_k), grow_v = shift_factor(was_v, now_v);
+            const int words = D / 4;
+            for (int u = lane; u < last * words; u += kWave) {
+                uint32_t *p = reinterpret_cast<uint32_t *>(granule(entry, u / words) + u / words % kKvGranule * D) + u % words;
+                *p = shift_codes(*p, grow_k);
+            }
+            for (int u = lane; u < (last + 3) / 4 * D; u += kWave) { // four slots of an element
+                const int t = u / D * 4;
+                uint32_t *p = reinterpret_cast<uint32_t *>(granule(entry, t) + kKvGranule * D + u % D * kKvGranule + t % kKvGranule);
+                const uint32_t old = *p, mask = t + 4 <= last ? 0xffffffffu : (1u << (8 * (last - t))) - 1;
+                *p = (shift_codes(old, grow_v) & mask) | (old & ~mask); // (the row is this wavefront's alone)
+            }
+            team_sync<1>(); // the moved tokens' bytes go over these
+        }
+#pragma unroll
+        for (int k = 0; k < kEvictFew; ++k) {
+            if (m0 + k >= m1) break;
+            const int t = move[m0 + k][1] - block * s.N;
+            uint8_t *g = granule(entry, t);
+            if (lane < D / 4) *(reinterpret_cast<uint32_t *>(g + t % kKvGranule * D) + lane) = shift_codes(k4[k], fk[k]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (lane + x * kWave < D) g[kKvGranule * D + (lane + x * kWave) * kKvGranule + t % kKvGranule] = (uint8_t)shift_codes(v1[k][x], fv[k]);
+        }
+        if (lane < 2) s.exps[2 * entry + lane] = (int8_t)(lane ? now_v : now_k);
+    }
+}
+
 // A workgroup = some of the blocks of a row (sequence and head) that keep tokens, those that take any.  Nobody writes slots from keep on,
 // and nobody else these blocks'.  A thread has 16 bytes of a token's K, or the eight tokens of a granule in one element
 // of V: what stays (shifted, if a larger exponent comes) and what comes are put together in registers.
@@ -1278,6 +1434,10 @@ int32_t launch_kv_evict(const slora_kv8_batch *b, const KvShape &shape, const Kv
 {
     const int64_t rows = (int64_t)b->seqs.size() * shape.n_kv;
     hipStream_t st = (hipStream_t)stream;
+    if (b->most_going <= kEvictFew && b->longest <= kEvictFewTokens) {
+        hipLaunchKernelGGL(kv_evict_few_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, b->d_seqs, (int)rows, shape, e);
+        return check_launch("kv_evict_few");
+    }
     auto select = [&](auto w) -> int32_t {
         typedef Evict<w.value> E;
         // stripes of the longest run, at most what LDS holds

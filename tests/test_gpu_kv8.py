@@ -297,6 +297,31 @@ def test_eviction_of_long_sequences_step_by_step():
             evict_and_check(t, [1, 0], [401, 401], 50, w, pos, in_place=True)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("D,H,dtype", [(32, 512, "f16"), (64, 512, "bf16"), (128, 4096, "f16"), (192, 1536, "f16"), (256, 2048, "bf16")])
+def test_eviction_of_a_few_tokens(D, H, dtype, in_place):
+    """none to four tokens over the budget, equal weights, tokens that are themselves behind it, blocks in smaller units than what comes"""
+    with Twin(H, D, 5, 1, dtype, max_seqs=6, max_tokens=400) as t:
+        for size in (0.05, 1.0, 9.0):
+            t.step([0, 1, 2, 3, 4, 5], [100, 3, 60, 61, 2, 110], size)
+        lens = list(t.len)
+        w, _, pos = t.weight_arrays()
+        w[t.rng.random(w.shape) < 0.5] = 0.0
+        w[2, 1] = 0.0
+        w[3, 2, :20], w[3, 2, 5] = float("nan"), -0.0
+        w[5, :, lens[5] - 4:] = 0.0  # the last ones go, or stay as recent
+        for s in range(6):
+            pos[s, :, :lens[s]] = torch.arange(lens[s], device="cuda", dtype=torch.int32)
+        keep = [lens[0] - 4, lens[1] - 1, lens[2] - 3, lens[3], lens[4] - 4, lens[5] - 2]
+        for recent in (0, 3):
+            w, pos = evict_and_check(t, [0, 1, 2, 3, 4, 5], keep, recent, w, pos, in_place)
+            t.step([0, 1, 2, 3, 4, 5], [4, 1, 3, 0, 2, 2], 20.0 * (recent + 1))
+            for s, n in enumerate([4, 1, 3, 0, 2, 2]):
+                w[s, :, t.len[s] - n:t.len[s]] = 0.125 * s
+                pos[s, :, t.len[s] - n:t.len[s]] = torch.arange(t.seen[s] - n, t.seen[s], device="cuda", dtype=torch.int32)
+        evict_and_check(t, [4, 1], [1, 0], 0, w, pos, in_place)
+
+
 def test_a_table_entry_that_is_given_another_page():
     """truncate, then grow again on other pages while earlier work may still run"""
     with Twin(512, 64, 1, 2, max_seqs=2, max_tokens=200) as t:
