@@ -440,7 +440,7 @@ int32_t slora_kv8_batch_plan(slora_kv8 *c, slora_kv8_batch **out, int32_t n, con
             b->most_going = std::max(b->most_going, s.len - s.keep);
             if (s.keep < s.len) {
                 b->moves += (int64_t)std::min(s.keep, s.len - s.keep) * c->n_kv;
-                b->firsts += (int64_t)(c->blocks(s.keep) + 1) * c->n_kv;
+                b->firsts += (int64_t)(c->blocks(s.keep) + 2) * c->n_kv;
                 b->dest_blocks = std::max(b->dest_blocks, c->blocks(s.keep));
             }
             const int64_t cols = (int64_t)rows[i] * (c->n_heads / c->n_kv);
@@ -576,7 +576,7 @@ int32_t slora_kv8_evict(slora_kv8_batch *b, int32_t layer, int32_t recent, const
     const slora_kv8 *c = b->cache;
     DeviceScope dev(c->pool->device);
     if (dev.status() != SLORA_OK) return dev.status();
-    rc = c->pool->grow_v(b->set, (size_t)(3 * b->moves + b->firsts), 0, stream);
+    rc = c->pool->grow_v(b->set, (size_t)(2 * b->moves + b->firsts), 0, stream);
     if (rc == SLORA_OK) rc = b->enter(stream);
     if (rc != SLORA_OK) return rc;
     KvEvict e{};
@@ -587,8 +587,7 @@ int32_t slora_kv8_evict(slora_kv8_batch *b, int32_t layer, int32_t recent, const
     e.recent = recent;
     e.src = reinterpret_cast<int32_t *>(b->set->v);
     e.dst = e.src + b->moves;
-    e.e = e.dst + b->moves;
-    e.first = e.e + b->moves;
+    e.first = e.dst + b->moves;
     return launch_kv_evict(b, shape_of(c, layer), e, stream);
 }
 

@@ -23,7 +23,7 @@ struct KvSeq {
     int32_t seen;      // positions given out
     int32_t keep;      // tokens that an eviction leaves
     int32_t move0;     // first entry of its list of moves, for head 0 (each head has min(keep, len - keep) of them)
-    int32_t first0;    // first entry of its counts of moves before each block, for head 0 (blocks + 1 each)
+    int32_t first0;    // first entry of its counts of moves before each block, for head 0 (blocks + 2 each)
     int64_t score0;    // first of its scores, [head][column][token] with tokens rounded up to 8; -1: more columns than have them kept
     int64_t pad;
 };
@@ -79,8 +79,8 @@ struct KvEvict {
     const int32_t *pos_in;
     int32_t *pos_out;
     int32_t recent;
-    int32_t *src, *dst, *e; // moves: from, to, exponents of the source (K in the low 16 bits, V above)
-    int32_t *first;         // moves before each block
+    int32_t *src, *dst; // moves: from, to
+    int32_t *first;     // moves before each block, all moves, exponents of the block about the budget
 };
 
 } // namespace slora

@@ -975,7 +975,12 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
             const int i = j + k * kWave + lane;
             const uint32_t r = rank_of(a[k], p[k], recent_from);
             if (i - lane < held && i - lane < n) ranks[i] = r;
-            count(bins, r >> (32 - kBits), i < n);
+            const uint32_t digit = r >> (32 - kBits), d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+            if (__ballot(digit != d0) == 0) { // (recent tokens, tokens that drew nothing; lanes behind the last slot have the last one's)
+                if (lane == 0) atomicAdd(&bins[place(d0)], (uint32_t)max(min(n - (i - lane), kWave), 0));
+            } else if (i < n) {
+                atomicAdd(&bins[place(digit)], 1u);
+            }
             if (copies && i < n && lo + i < q.keep) { // (places that fall free are written again, by what moves there)
                 e.w_out[at + lo + i] = a[k];
                 e.pos_out[at + lo + i] = p[k];
@@ -1058,8 +1063,8 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
     }
     const uint64_t lower = (uint64_t(1) << lane) - 1;
     const int most = min(q.keep, q.len - q.keep), blocks = (q.keep + s.N - 1) / s.N;
-    int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
-    int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
+    int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most;
+    int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 2);
     walk([&](int i, uint32_t r, bool in) {
         const uint64_t same = __ballot(in && r == prefix);
         const bool stays = in && (r > prefix || (r == prefix && seen + (int)__popcll(same & lower) < left));
@@ -1080,13 +1085,15 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
         if (move) {
             const int m = moves + (int)__popcll(ms & lower);
             src[m] = i;
-            const int16_t both = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, i / s.N, head)];
-            ex[m] = ((int32_t)(int8_t)(both & 0xff) & 0xffff) | ((int32_t)(both >> 8) << 16);
         }
         moves += (int)__popcll(ms);
     });
     if constexpr (W == 1) total = moves;
-    if (wave == 0 && lane == 0) first[blocks] = total;
+    if (wave == 0 && lane == 0) {
+        first[blocks] = total;
+        // the exponents of the block about the budget, from which tokens move and into which tokens move
+        first[blocks + 1] = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, q.keep / s.N, head)];
+    }
     team_sync<W>();
     // (entries of slots from keep on are only read)
     for (int m = wave * kWave + lane; m < total; m += W * kWave) {
@@ -1257,8 +1264,13 @@ __global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq
     const int head = blockIdx.x % s.n_kv, D = s.D, lane = threadIdx.x % kWave;
     const int blocks = (q.keep + s.N - 1) / s.N;
     const int most = min(q.keep, q.len - q.keep);
-    const int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most, *ex = e.e + q.move0 + (int64_t)head * most;
-    const int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 1);
+    const int32_t *src = e.src + q.move0 + (int64_t)head * most, *dst = e.dst + q.move0 + (int64_t)head * most;
+    const int32_t *first = e.first + q.first0 + (int64_t)head * (blocks + 2);
+    // exponents of a source, K's in the low byte: of blocks behind the budget, which nobody changes, or as the block about it had them
+    auto exponents_of = [&](int slot) {
+        const int b = (int)kv_div((uint32_t)slot / kKvGranule, s.div_b);
+        return b == q.keep / s.N ? first[blocks + 1] : (int)reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, b, head)];
+    };
     const int granule_bytes = 2 * kKvGranule * D;
     // blocks y, y + gridDim.y, ...: 64 at a time
     for (int k0 = 0; (int)blockIdx.y + k0 * (int)gridDim.y < blocks; k0 += kWave) {
@@ -1273,8 +1285,9 @@ __global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq
             const int was_k = s.exps[2 * entry], was_v = s.exps[2 * entry + 1];
             int now_k = was_k, now_v = was_v;
             for (int m = m0 + lane; m < m1; m += kWave) {
-                now_k = max(now_k, (int)(int16_t)(ex[m] & 0xffff));
-                now_v = max(now_v, ex[m] >> 16);
+                const int both = exponents_of(src[m]);
+                now_k = max(now_k, (int)(int8_t)(both & 0xff));
+                now_v = max(now_v, both >> 8);
             }
 #pragma unroll
             for (int x = 32; x; x >>= 1) {
@@ -1293,12 +1306,12 @@ __global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq
             }
             __syncthreads();
             for (int m = m0 + (int)threadIdx.x; m < m1; m += kMoveThreads) {
-                const int t = dst[m] - block * s.N, from = src[m], r = from % s.N;
+                const int t = dst[m] - block * s.N, from = src[m], r = from % s.N, both = exponents_of(from);
                 const uint8_t *there = granule(s.pool + (int64_t)s.table[table_entry(s, q.seq, from / s.N, head)] * s.page_bytes, r);
                 from_k[t] = there + (r % kKvGranule) * D;
                 from_v[t] = there + kKvGranule * D + r % kKvGranule;
-                factor[0][t] = shift_factor((int)(int16_t)(ex[m] & 0xffff), now_k);
-                factor[1][t] = shift_factor(ex[m] >> 16, now_v);
+                factor[0][t] = shift_factor((int8_t)(both & 0xff), now_k);
+                factor[1][t] = shift_factor(both >> 8, now_v);
                 comes[t] = 1;
             }
             __syncthreads();
