@@ -603,24 +603,41 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
         if (more) fetch(g + kManyGranules);
         const int first = g * kKvGranule;
         if (first < any_sees) {
+            // Operands are read a group of steps ahead of the products that take them (left to itself the compiler reads each one right before,
+            // and waits), and the halves take turns, so that a product does not wait for the one before.
             f32x16 sc[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+            constexpr int kGroup = 2, kGroups = kSteps / kGroup;
+            f16x8 kf[2][kGroup][2];
+            auto read_k = [&](int j0, f16x8 (&to)[kGroup][2]) {
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) { // unit 2 j + h: c = j
-                    const f16x8 kf = __builtin_bit_cast(f16x8, lds.k[buffer][(2 * j + h) * kManyTile + ((t * 32 + token_n) ^ (j % 2 * 8))]);
-                    sc[t] = mfma32(kf, qf[j], sc[t]);
-                }
+                for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) // unit 2 j + h: c = j
+                        to[j][t] = __builtin_bit_cast(f16x8, lds.k[buffer][(2 * (j0 + j) + h) * kManyTile + ((t * 32 + token_n) ^ ((j0 + j) % 2 * 8))]);
+            };
+            read_k(0, kf[0]);
+#pragma unroll
+            for (int b = 0; b < kGroups; ++b) {
+                if (b + 1 < kGroups) read_k((b + 1) * kGroup, kf[(b + 1) % 2]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) sc[t] = mfma32(kf[b % 2][j][t], qf[b * kGroup + j], sc[t]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            // registers 8 s .. 8 s + 7 of half t: granule 4 t + 2 s + h
+            // registers 8 s .. 8 s + 7 of half t: granule 4 t + 2 s + h.  Scores from here on are less the maximum so far.
+            const float so_far = m == -INFINITY ? 0.0f : m;
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const float f = unit * lds.unit[buffer][4 * t + 2 * r + h], add = lds.add[buffer][4 * t + 2 * r + h];
+                    const float f = unit * lds.unit[buffer][4 * t + 2 * r + h], add = lds.add[buffer][4 * t + 2 * r + h] - so_far;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sc[t][8 * r + i] = __builtin_fmaf(sc[t][8 * r + i], f, add);
                 }
@@ -637,16 +654,21 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
             top = fmaxf(top, across_32(top));
-            if (__any(top > m + kSlack || (m == -INFINITY && top > m))) {
-                const float m_new = fmaxf(m, top), keep = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+            const bool raise = top > kSlack || (m == -INFINITY && top > -INFINITY);
+            if (__any(raise)) {
+                const float by = raise ? top : 0.0f, m_new = raise ? so_far + by : m;
+                const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by); // (nothing has been added up before the first maximum)
                 m = m_new;
                 l *= keep;
 #pragma unroll
                 for (int k = 0; k < DB; ++k)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[k][i] *= keep;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sc[t][i] -= by;
             }
-            const float use = m == -INFINITY ? 0.0f : m;
             f16x8 p[2][2];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -655,7 +677,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float x = __builtin_amdgcn_exp2f(sc[t][8 * r + i] - use);
+                        const float x = __builtin_amdgcn_exp2f(sc[t][8 * r + i]);
                         sum += x;
                         p[t][r][i] = (_Float16)x;
                     }
