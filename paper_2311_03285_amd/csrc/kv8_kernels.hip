@@ -497,8 +497,8 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
 // rows 8 b + 4 h + i of column n (register 4 b + i).
 //
 // A workgroup = an item of up to 128 columns, 32 to a wavefront, that walk the tokens in tiles of 64 together.  A tile's codes are turned into
-// binary16 once, on the way into LDS: K in units of 8 elements of a token, [unit][token] (tokens 8 apart change places in every
-// other pair of units, for the sake of the writes), V in units of 8 tokens of an element as its granules hold them - so that every
+// binary16 once, on the way into LDS: K in units of 8 elements of a token, [unit][token] (tokens of a granule change
+// places from one pair of units to the next, so that the eight lanes that write a token are in different banks), V in units of 8 tokens of an element as its granules hold them - so that every
 // operand is one read of 16 bytes, lane by lane in order.  While one tile is worked on, the next one's loads are under way; it
 // goes into the other buffer afterwards, and one barrier ends the round.
 //
@@ -557,6 +557,8 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
         for (int i = 0; i < 16; ++i) o[k][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
 
+    // eight lanes that write every other unit are in different banks
+    auto v_place = [](int unit) { return unit ^ (unit >> 3 & 1); };
     // a tile's pieces of 16 bytes, D to a granule (K's first), 256 at a time
     u32x4 raw[DB];
     auto fetch = [&](int g) {
@@ -573,13 +575,13 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
             const int u = threadIdx.x + i * kKvManyThreads, w = u % D;
             const u32x4 lo = __builtin_bit_cast(u32x4, codes_to_f16x8(raw[i].x, raw[i].y)), hi = __builtin_bit_cast(u32x4, codes_to_f16x8(raw[i].z, raw[i].w));
             if (w < D / 2) { // 16 elements of a token: units 2 c, 2 c + 1
-                const int token = u / D * kKvGranule + w / (D / 16), c = w % (D / 16), at = token ^ (c % 2 * 8);
+                const int token = u / D * kKvGranule + w / (D / 16), c = w % (D / 16), at = token ^ (c % 8);
                 lds.k[buffer][2 * c * kManyTile + at] = lo;
                 lds.k[buffer][(2 * c + 1) * kManyTile + at] = hi;
             } else { // two elements' eight tokens
                 const int at = u / D * D + 2 * (w - D / 2);
-                lds.v[buffer][at] = lo;
-                lds.v[buffer][at + 1] = hi;
+                lds.v[buffer][v_place(at)] = lo;
+                lds.v[buffer][v_place(at + 1)] = hi;
             }
         }
         if (threadIdx.x < kManyGranules) {
@@ -617,7 +619,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
                 for (int j = 0; j < kGroup; ++j)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) // unit 2 j + h: c = j
-                        to[j][t] = __builtin_bit_cast(f16x8, lds.k[buffer][(2 * (j0 + j) + h) * kManyTile + ((t * 32 + token_n) ^ ((j0 + j) % 2 * 8))]);
+                        to[j][t] = __builtin_bit_cast(f16x8, lds.k[buffer][(2 * (j0 + j) + h) * kManyTile + t * 32 + (token_n ^ ((j0 + j) % 8))]);
             };
             read_k(0, kf[0]);
 #pragma unroll
@@ -689,7 +691,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int k = 0; k < DB; ++k)
-                        o[k] = mfma32(__builtin_bit_cast(f16x8, lds.v[buffer][(4 * t + 2 * r + h) * D + 32 * k + n]), p[t][r], o[k]);
+                        o[k] = mfma32(__builtin_bit_cast(f16x8, lds.v[buffer][(4 * t + 2 * r + h) * D + 32 * k + v_place(n)]), p[t][r], o[k]);
         }
         if (more) put(buffer ^ 1, g + kManyGranules);
         __syncthreads();
