@@ -114,15 +114,15 @@ __device__ __forceinline__ int token_of_row(int m) { return 4 * (m % 4) + m / 4;
 // the wavefront's number in its workgroup, as a scalar
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave); }
 
-// Few tokens (TI = 1: up to four; 4: up to 16).  A workgroup = RT tiles of 16 outputs; its WV wavefronts take chunks of 128 inputs in turn, with the weights of the next ones and x of the
+// Up to four tokens.  A workgroup = RT tiles of 16 outputs; its WV wavefronts take chunks of 128 inputs in turn, with the weights of the next ones and x of the
 // next one under way, and are added in LDS.  Loads are not behind branches where others are waited for: the compiler would wait for all of them.
-template <int DT, int RT, int WV, int TI, int U>
+template <int DT, int RT, int WV, int U>
 __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
 {
     typedef typename Operand<DT>::type operand;
     constexpr int kPer = kW4Chunk / U; // units of a chunk
     constexpr int kAhead = RT * kPer > 4 ? 2 : 4; // chunks of weights under way
-    __shared__ float part[WV][4 * TI][RT * 16];
+    __shared__ float part[WV][4][RT * 16];
     int k = 0;
     while (k + 1 < a.n && (int)blockIdx.x >= a.m[k + 1].first) ++k;
     const W4Matrix &m = a.m[k];
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
     const int tile0 = ((int)blockIdx.x - m.first) * RT;
     const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
 
-    float sum[RT][TI] = {}; // of tokens 4 i + g
+    float sum[RT] = {}; // of token g
     // (rows beyond the last token: the last once more, whose sums nobody takes)
     const uint16_t *const row = m.x + (int64_t)min(token_of_row(n), a.T - 1) * inputs;
     const uint8_t *const codes = m.codes, *const zeros = m.zeros;
@@ -176,8 +176,7 @@ __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
                     acc = Operand<DT>::mfma(xo, Operand<DT>::codes(now.w[r][s]), acc);
                     acc = Operand<DT>::mfma(xo, z, acc);
                 }
-#pragma unroll
-                for (int i = 0; i < TI; ++i) sum[r][i] = __builtin_fmaf(acc[i], widen<DT>(now.scale[r][u]), sum[r][i]);
+                sum[r] = __builtin_fmaf(acc[0], widen<DT>(now.scale[r][u]), sum[r]);
             }
     };
     if (wave < chunks) {
@@ -209,9 +208,7 @@ __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
         }
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < TI; ++i) part[wave][4 * i + g][r * 16 + n] = sum[r][i];
+    for (int r = 0; r < RT; ++r) part[wave][g][r * 16 + n] = sum[r];
     __syncthreads();
     for (int i = threadIdx.x; i < RT * 16 * a.T; i += WV * kWave) {
         const int r = i % (RT * 16), t = i / (RT * 16), o = tile0 * kW4Rows + r;
@@ -242,11 +239,13 @@ __device__ __forceinline__ void lds_barrier()
 }
 
 template <int DT, int TEAMS, int RT, int NT, int U>
-__global__ __launch_bounds__(kWideThreads) void w4_wide_kernel(W4Args a, bool y16)
+__global__ __launch_bounds__(kWideThreads, TEAMS == 2 && RT == 1 && NT <= 2 && (U > 32 || NT == 1) ? 6 : 2) void w4_wide_kernel(W4Args a, bool y16)
 {
     typedef typename Operand<DT>::type operand;
     constexpr int kPer = kW4Chunk / U, kRows = NT * 16, kPieces = kW4Chunk / 8;
-    constexpr int kAhead = 4; // chunks of weights under way
+    // Chunks of weights under way.  Two, and with them registers for three workgroups of a compute unit, are as fast as four and two workgroups, or faster: two of
+    // 20480 of 5120, 32 tokens 44.4 -> 39.2 us, where two at a time go through 640 workgroups in one round and a quarter.
+    constexpr int kAhead = 2;
     constexpr int kMembers = 8 / TEAMS;     // wavefronts of a team,
     constexpr int kPuts = NT * 4 / kMembers; // each of which puts four rows at a time into LDS, so often
     constexpr int kStage = kRows * kPieces, kMerge = 8 * RT * NT * kWave; // pieces of 16 bytes
@@ -413,11 +412,11 @@ int64_t share_out(W4Args &a, int each)
     return groups;
 }
 
-template <int DT, int RT, int WV, int TI, int U>
+template <int DT, int RT, int WV, int U>
 int32_t launch(W4Args &a, bool y16, void *stream)
 {
     const int64_t groups = share_out(a, RT);
-    hipLaunchKernelGGL((w4_kernel<DT, RT, WV, TI, U>), dim3((unsigned)groups), dim3(WV * kWave), 0, (hipStream_t)stream, a, y16);
+    hipLaunchKernelGGL((w4_kernel<DT, RT, WV, U>), dim3((unsigned)groups), dim3(WV * kWave), 0, (hipStream_t)stream, a, y16);
     return check_launch("w4");
 }
 
@@ -449,8 +448,8 @@ int32_t wide(W4Args &a, int64_t tiles, bool y16, void *stream)
     return launch_wide<DT, 2, 1, NT, U>(a, y16, stream);
 }
 
-// Up to 16 tokens of few outputs read x for themselves.  us, w4_kernel / w4_wide_kernel: 4096 of 4096, one token 4.8 / 6.0, 16 tokens 6.6 / 7.4, 8192 of 8192,
-// 16 tokens 12.4 / 18.4; four of 4096 of 4096, one token 9.8 / 11.9, 16 tokens 12.6 / 12.0; two of 20480 of 5120, 16 tokens 38.7 / 30.0.
+// Up to four tokens read x for themselves.  us, w4_kernel / w4_wide_kernel: 4096 of 4096, one token 4.8 / 6.0, 8192 of 8192 9.8 / 12.0, four of 4096 of
+// 4096 9.8 / 11.9, two of 20480 of 5120 28.0 / 27.0; of 8 tokens the second one is as fast or faster (8192 of 8192 14.4 / 12.9).
 template <int DT, int U>
 int32_t by_tokens(W4Args &a, bool y16, void *stream)
 {
@@ -459,11 +458,10 @@ int32_t by_tokens(W4Args &a, bool y16, void *stream)
     if (a.T <= 4) {
         // two tiles share x; us with one / two: 4096 of 4096 4.7 / 5.5, 8192 of 8192 10.4 / 9.3; eight / four wavefronts: two of 20480 of 5120 33.5 / 28.0,
         // four of 4096 of 4096 9.4 / 10.1
-        if (tiles >= 2048) return launch<DT, 2, 4, 1, U>(a, y16, stream);
-        if (tiles >= 512) return launch<DT, 2, 8, 1, U>(a, y16, stream);
-        return launch<DT, 1, 8, 1, U>(a, y16, stream);
+        if (tiles >= 2048) return launch<DT, 2, 4, U>(a, y16, stream);
+        if (tiles >= 512) return launch<DT, 2, 8, U>(a, y16, stream);
+        return launch<DT, 1, 8, U>(a, y16, stream);
     }
-    if (a.T <= 16 && tiles <= 512) return launch<DT, 1, 8, 4, U>(a, y16, stream);
     const int32_t rows = (a.T - 1) / 16 + 1, blocks = (rows + 3) / 4;
     switch ((rows + blocks - 1) / blocks) {
     case 1: return wide<DT, U, 1>(a, tiles, y16, stream);
