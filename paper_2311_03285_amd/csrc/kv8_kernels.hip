@@ -819,69 +819,134 @@ __global__ __launch_bounds__(256) void kv_weights_few_kernel(const KvSeq *__rest
     out.w_out[at] = v;
 }
 
-// The scores once more, 32 tokens a wavefront, with the maxima and sums that attention left; a lane adds up its tokens over its column of
-// every tile, then the 16 columns are added.
+// ... of many columns: the scores once more, from the maxima and sums that attention left.  A wavefront has the K of 32 tokens in registers (row
+// 8 b + 4 h + i of the 32 x 32 instruction is its token of that number, of granule b); the workgroup's four go through the columns together,
+// 32 at a time, which are put into LDS as binary16 while the ones before are worked on.  A lane adds up its tokens over its column of
+// every tile; the 32 columns are added at the end.
+template <int DB>
+struct WeightsLds {
+    u32x4 q[2][DB * 4 * 32]; // [8 elements][column]
+    float unit[2][32], m[2][32], by[2][32]; // of each column: what its scores are multiplied by, maximum, 1 / sum
+    int limit[2][32];                       // tokens it sees
+};
 template <int DT, int DB>
-__global__ __launch_bounds__(kKvFewThreads) void kv_weights_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvAttend a, KvWeights out)
+__global__ __launch_bounds__(256) void kv_weights_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvAttend a, KvWeights out)
 {
-    constexpr int D = DB * 32, kWaves = kKvFewThreads / kWave;
+    constexpr int D = DB * 32, kSteps = 2 * DB;
+    __shared__ WeightsLds<DB> lds;
     const KvSeq q = seqs[blockIdx.z];
     if (q.score0 >= 0) return; // (kv_weights_few_kernel's)
-    const int head = blockIdx.y;
-    const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
-    const int gr = (blockIdx.x * kWaves + wave) * (kKvChunk / kKvGranule), granules = (q.len + kKvGranule - 1) / kKvGranule;
-    if (gr >= granules) return;
-    const int gpb = s.N / kKvGranule, old = q.len - q.rows;
-    u32x4 kr[2][(DB + 1) / 2];
-    const int gk = min(gr + n / 4, granules - 1), gv = min(gr + g, granules - 1);
-    const uint8_t *pk = s.pool + (int64_t)s.table[table_entry(s, q.seq, gk / gpb, head)] * s.page_bytes + (int64_t)(gk % gpb) * (2 * kKvGranule * D) + (n % 4) * D;
-    load_k<DB>(pk, g, kr[0]);
-    load_k<DB>(pk + 4 * D, g, kr[1]);
-    const int ek = s.exps[2 * table_entry(s, q.seq, gv / gpb, head)];
-    f16x8 kf[2][DB];
+    const int head = blockIdx.y, wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 32, h = lane / 32;
+    const int first = blockIdx.x * 128, token0 = first + wave * 32, granules = (q.len + kKvGranule - 1) / kKvGranule;
+    if (first >= q.len) return;
+    const int gpb = s.N / kKvGranule, old = q.len - q.rows, cols = q.rows * s.G;
+    f16x8 kf[kSteps];
+    float f[4];
+    {
+        auto block_of = [&](int g) { return (int)kv_div((uint32_t)g, s.div_b); };
+        const int g = min(token0 / kKvGranule + n / kKvGranule, granules - 1), b = block_of(g);
+        const uint8_t *row = s.pool + (int64_t)s.table[table_entry(s, q.seq, b, head)] * s.page_bytes + (int64_t)(g - b * gpb) * (2 * kKvGranule * D) + n % kKvGranule * D;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < DB; ++j) kf[t][j] = k_operand<DB>(kr[t], j);
-    const int token = (gr + g) * kKvGranule, cols = q.rows * s.G;
-    float w[8] = {};
-    // rows before the chunk's first token see none of it
-    for (int c0 = a.causal ? max(gr * kKvGranule - old, 0) * s.G / 16 * 16 : 0; c0 < cols; c0 += 16) {
-        const int col = c0 + n, row = col / s.G, h = head * s.G + col % s.G;
-        const bool real = col < cols;
-        f16x8 qf[DB];
-        float unit;
-        load_q<DT, DB>(real ? a.q + (int64_t)(q.row0 + row) * a.q_stride + (int64_t)h * D : nullptr, g, qf, unit);
-        const float *st = a.stat + 2 * ((int64_t)(q.row0 + row) * s.n_kv * s.G + h);
-        const float m = real ? st[0] : 0.0f, by = real ? st[1] : 0.0f;
-        const float f = unit * a.scale * unit_of(ek);
-        const int bound = (!real ? 0 : a.causal ? min(old + row + 1, q.len) : q.len) - token;
-        f32x4 sc[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            sc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int j = 0; j < DB; ++j) sc[t] = mfma16(kf[t][j], qf[j], sc[t]);
+        for (int j = 0; j < kSteps; ++j) {
+            const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 16 * j + 8 * h);
+            kf[j] = codes_to_f16x8(u.x, u.y);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < bound) w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 4][i % 4], f, -m)), by, w[i]);
+        for (int k = 0; k < 4; ++k) f[k] = unit_of(s.exps[2 * table_entry(s, q.seq, block_of(min(token0 / kKvGranule + k, granules - 1)), head)]);
+    }
+    // columns change places by the eighth of the elements that a unit is of: the eight threads that write a column are in different banks
+    auto turn = [](int unit) { return unit * 64 / D % 8; };
+    // a thread's share of a tile of columns: an eighth of one of them
+    const int column = threadIdx.x / 8, part = threadIdx.x % 8;
+    u32x2 raw[DB];
+    float m_next = 0.0f, by_next = 0.0f;
+    int limit_next = 0;
+    auto fetch = [&](int c0) {
+        const int col = c0 + column, row = col / s.G, qhead = head * s.G + col % s.G;
+        const bool real = col < cols;
+        const uint16_t *x = a.q + (int64_t)(q.row0 + (real ? row : 0)) * a.q_stride + (int64_t)(real ? qhead : head * s.G) * D + part * (D / 8);
+#pragma unroll
+        for (int k = 0; k < DB; ++k) raw[k] = real ? *reinterpret_cast<const u32x2 *>(x + 4 * k) : u32x2{0u, 0u};
+        const float *st = a.stat + 2 * ((int64_t)(q.row0 + (real ? row : 0)) * s.n_kv * s.G + (real ? qhead : head * s.G));
+        m_next = real ? st[0] : 0.0f;
+        by_next = real ? st[1] : 0.0f;
+        limit_next = !real ? 0 : a.causal ? min(old + row + 1, q.len) : q.len;
+    };
+    auto put = [&](int buffer) {
+        float unit = 1.0f, scale = 1.0f;
+        if constexpr (DT == SLORA_BF16) { // as load_column
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < DB; ++k) top = max(max(top, max(raw[k].x & 0x7fffu, (raw[k].x >> 16) & 0x7fffu)), max(raw[k].y & 0x7fffu, (raw[k].y >> 16) & 0x7fffu));
+#pragma unroll
+            for (int x = 1; x < 8; x *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, x, kWave));
+            const int x = (int)(top >> 7), up = x == 0 || x == 255 ? 0 : min(max(141 - x, -100), 100);
+            scale = __uint_as_float((uint32_t)(127 + up) << 23);
+            unit = __uint_as_float((uint32_t)(127 - up) << 23);
+        }
+#pragma unroll
+        for (int k = 0; k < DB; ++k) { // elements e .. e + 3
+            const int e = part * (D / 8) + 4 * k;
+            u32x2 v = raw[k];
+            if constexpr (DT == SLORA_BF16) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+                    v[w] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)(__uint_as_float(raw[k][w] << 16) * scale), (_Float16)(__uint_as_float(raw[k][w] & 0xffff0000u) * scale)});
+            }
+            reinterpret_cast<u32x2 *>(&lds.q[buffer][e / 8 * 32 + (column ^ turn(e / 8))])[e / 4 % 2] = v;
+        }
+        if (part == 0) {
+            lds.unit[buffer][column] = unit * a.scale;
+            lds.m[buffer][column] = m_next;
+            lds.by[buffer][column] = by_next;
+            lds.limit[buffer][column] = limit_next;
+        }
+    };
+    float w[16] = {};
+    // rows before the workgroup's first token see none of its tokens
+    int c0 = a.causal ? max(first - old, 0) * s.G / 32 * 32 : 0, buffer = 0;
+    if (c0 < cols) {
+        fetch(c0);
+        put(0);
+    }
+    __syncthreads();
+    for (; c0 < cols; c0 += 32, buffer ^= 1) {
+        if (c0 + 32 < cols) fetch(c0 + 32);
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) sc = mfma32(kf[j], __builtin_bit_cast(f16x8, lds.q[buffer][(2 * j + h) * 32 + (n ^ turn(2 * j + h))]), sc);
+        const float unit = lds.unit[buffer][n], m = lds.m[buffer][n], by = lds.by[buffer][n];
+        const int limit = lds.limit[buffer][n];
+        const bool all_seen = __all(limit >= token0 + 32 || by == 0.0f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * k + i], unit * f[k], -m));
+                if (!all_seen) p = token0 + 8 * k + 4 * h + i < limit ? p : 0.0f;
+                w[4 * k + i] = __builtin_fmaf(p, by, w[4 * k + i]);
+            }
+        if (c0 + 32 < cols) put(buffer ^ 1);
+        __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 16; ++i)
 #pragma unroll
-        for (int x = 8; x; x >>= 1) w[i] += __shfl_xor(w[i], x, kWave);
-    if (n < 8 && token + n < q.len) {
-        float v = 0.0f;
+        for (int x = 16; x; x >>= 1) w[i] += __shfl_xor(w[i], x, kWave);
+    if (n >= 16) return;
+    float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v = n == i ? w[i] : v;
-        const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens + token + n;
-        if (token + n < old)
-            v += out.w_in[at];
-        else
-            out.pos[at] = q.seen - q.rows + token + n - old;
-        out.w_out[at] = v;
-    }
+    for (int i = 0; i < 16; ++i) v = n == i ? w[i] : v;
+    const int token = token0 + 8 * (n / 4) + 4 * h + n % 4;
+    if (token >= q.len) return;
+    const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens + token;
+    if (token < old)
+        v += out.w_in[at];
+    else
+        out.pos[at] = q.seen - q.rows + token - old;
+    out.w_out[at] = v;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1459,10 +1524,9 @@ int32_t launch_kv_weights(const slora_kv8_batch *b, const KvShape &shape, const 
         int32_t rc = check_launch("kv_weights_few");
         if (rc != SLORA_OK || b->longest_many == 0) return rc;
     }
-    const int per = kKvFewThreads / kWave * kKvChunk;
-    const dim3 grid((unsigned)((b->longest_many + per - 1) / per), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
+    const dim3 grid((unsigned)((b->longest_many + 127) / 128), (unsigned)shape.n_kv, (unsigned)b->seqs.size());
     return by_shape(b->cache->pool->dtype, shape.D, [&](auto dt, auto db) {
-        hipLaunchKernelGGL((kv_weights_kernel<dt.value, db.value>), grid, dim3(kKvFewThreads), 0, (hipStream_t)stream, b->d_seqs, shape, a, w);
+        hipLaunchKernelGGL((kv_weights_kernel<dt.value, db.value>), grid, dim3(256), 0, (hipStream_t)stream, b->d_seqs, shape, a, w);
         return check_launch("kv_weights");
     });
 }
