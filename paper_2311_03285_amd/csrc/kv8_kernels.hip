@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256) void kv_table_kernel(int32_t *__restrict__ tab
 // they are in the caches): once for the largest value, once to round them.  K: 16 bytes of a row a lane.  V, which is
 // stored transposed: a lane has two elements of the eight tokens of a granule, reads them as 4 bytes of eight rows and writes
 // 16 bytes; what the granule held before stays, in new units if the exponent has grown.
+// Bound: latency (item, page, rows, sum, store in turn); one token of 64 sequences x 8 heads 4.9 us, 512 tokens x 32 heads 8.0 us = 1.6 TB/s.
 template <int DT>
 __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAppend a)
 {
@@ -320,6 +321,9 @@ __device__ __forceinline__ void load_pages(PartPages &pp, const KvShape &s, int 
 
 // A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
 // maxima, sums and O', and are put together in LDS at the end.
+// Bound: HBM, from which the cache comes once, with non-temporal loads (645 MB of 64 sequences, 8 heads: 115 us = 5.6 TB/s, with plain loads 125; 227 MB of
+// 24 sequences, 40 heads: 46 us = 4.9 TB/s); a single sequence of 701 tokens takes 5.3 us, the chain of page, K, score, sum.  Matrix and vector
+// units are under a third busy even with one column in use of sixteen, so there is no kernel of its own for one.
 template <int DT, int DB>
 __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
@@ -511,6 +515,9 @@ __device__ __forceinline__ f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f
 constexpr int kManyTile = kKvManyTile, kManyGranules = kManyTile / kKvGranule;
 constexpr float kSlack = 8.0f;
 
+// Bound: the vector units (56 % busy; 12.8 vector instructions for each of the 32 cycles of a matrix instruction, half of them the softmax's, a sixth the codes'),
+// beside the matrix units (35 %): a chunk of 512 behind 30000 tokens, 64 heads 627 us = 810 TFLOP/s, chunks of 128 - 1024 behind up to 4096 426 us.
+// Two workgroups share a compute unit up to 128 elements a head, so that one's products run beside the other's softmax.
 template <int DB>
 struct ManyLds {
     static constexpr int kUnits = kManyTile * DB * 4; // of 16 bytes, K's or V's of a tile
@@ -730,6 +737,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
 
 // Parts of a column put together, in the order of the sequence.  W = 4: a workgroup per column, whose wavefronts take parts in turn and are
 // added in LDS; W = 1, where there are few parts: a wavefront per column.
+// Bound: latency; 24 x 40 columns of up to 4 parts 4.7 us, 16 x 8 of up to 64 parts 8.4 us.
 template <int DT, int DB, int W>
 __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
@@ -797,6 +805,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__
 // ---------------------------------------------------------------------------------------
 // ... from scores that attention left, of sequences with few columns: a thread per token.  Scores of tokens that a column does not see, and of
 // those behind the last that any sees, are not read.
+// 24 sequences of 200 - 1500 tokens, 40 heads 6.0 us; computed again from K (as kv_weights_kernel does) it was 36.
 __global__ __launch_bounds__(256) void kv_weights_few_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvAttend a, KvWeights out)
 {
     const KvSeq q = seqs[blockIdx.z];
@@ -823,6 +832,7 @@ __global__ __launch_bounds__(256) void kv_weights_few_kernel(const KvSeq *__rest
 // 8 b + 4 h + i of the 32 x 32 instruction is its token of that number, of granule b); the workgroup's four go through the columns together,
 // 32 at a time, which are put into LDS as binary16 while the ones before are worked on.  A lane adds up its tokens over its column of
 // every tile; the 32 columns are added at the end.
+// Bound: vector units (an exponential and two products for each score); a chunk of 512 behind 30000 tokens, 64 heads 510 us beside attention's 627.
 template <int DB>
 struct WeightsLds {
     u32x4 q[2][DB * 4 * 32]; // [8 elements][column]
@@ -979,6 +989,8 @@ __device__ __forceinline__ void team_sync()
 // LDS, and every wavefront finds the digit from the counts for itself - lane l has the bins of digits B l .. B l + B - 1, digit B l + k
 // at place 64 k + l.  Then the counts of each run say where its places and moves go in the lists: all
 // integers, in the order of the slots.
+// Wavefronts: one for rows of up to 2048 tokens where there are many rows, four for up to 8192, else sixteen.  Bound: vector instructions of the one compute unit that a
+// row has; 64 rows of 8000 - 32000 tokens 45 us.
 template <int W>
 struct Evict {
     static constexpr int kThreads = W == 1 ? 256 : W * kWave, kTeams = kThreads / kWave / W;
@@ -1194,6 +1206,8 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
 // A cache at its budget, which has few tokens more than it keeps after each step: a wavefront per row, in one launch.  The token that goes is the one of
 // least rank, of equal ones that in the highest slot; the next one is the least behind it in this order.  What stays of
 // the slots behind the budget moves at once.
+// 64 sequences x 32 heads of 1025 tokens 13 us, 26 MB of weights and positions read and written; kv_evict_select_kernel and kv_evict_move_kernel took 36.
+// Bound: the latency of a pass over the row by one wavefront and then of the move.
 constexpr int kEvictFew = 4, kEvictFewTokens = 8192;
 __global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restrict__ seqs, int n_rows, KvShape s, KvEvict e)
 {
@@ -1340,6 +1354,7 @@ __global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restri
 // A workgroup = some of the blocks of a row (sequence and head) that keep tokens, those that take any.  Nobody writes slots from keep on,
 // and nobody else these blocks'.  A thread has 16 bytes of a token's K, or the eight tokens of a granule in one element
 // of V: what stays (shifted, if a larger exponent comes) and what comes are put together in registers.
+// Bound: V's bytes, a line of which holds 16 elements of eight tokens; 64 rows that take about 1900 tokens each 34 us.
 constexpr int kMoveThreads = 256;
 __global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq *__restrict__ seqs, KvShape s, KvEvict e)
 {
