@@ -13,7 +13,9 @@ constexpr int kKvFewThreads = 256;   // 4 wavefronts, which take turns at chunks
 constexpr int kKvChunk = 32;
 constexpr int kKvManyTile = 64;      // tokens that a workgroup of prompts takes at a time
 constexpr int kKvManyCols = 128, kKvManyThreads = 256; // columns of a workgroup of prompts: 32 for each of four wavefronts
-constexpr int kKvManyFrom = 33;      // columns of a sequence from which it is one
+// Columns of a sequence from which it is one.  us a pass, tiles of 16 / of 128: 24 columns of 8 sequences, 32 cached heads, behind 1000 tokens 41 / 35, 48 there 52 / 45;
+// 32 columns of 32 sequences, 8 cached heads, behind 2000 48 / 57, 64 there 64 / 67: with 33 neither loses more than a sixth.
+constexpr int kKvManyFrom = 33;
 constexpr int kKvPartBlocks = 512;   // most blocks of a part of a sequence: their page numbers are held in LDS
 
 // a sequence of the batch

@@ -280,19 +280,19 @@ __device__ __forceinline__ void load_q32(const uint16_t *q, int h, f16x8 (&f)[2 
     load_column<DT, 2 * DB, 32>(q, [=](int j) { return 16 * j + 8 * h; }, f, unit);
 }
 
-// K of one token as first operands, from its row
-template <bool NT>
+// (the cache is read once)
 __device__ __forceinline__ u32x4 load_once(const uint8_t *p)
 {
-    return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)) : *reinterpret_cast<const u32x4 *>(p);
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 }
-template <int DB, bool NT = false>
+// K of one token as first operands, from its row
+template <int DB>
 __device__ __forceinline__ void load_k(const uint8_t *row, int g, u32x4 (&raw)[(DB + 1) / 2])
 {
 #pragma unroll
     for (int p = 0; p < (DB + 1) / 2; ++p) {
         if (2 * p + 1 < DB) {
-            raw[p] = load_once<NT>(row + 64 * p + 16 * g);
+            raw[p] = load_once(row + 64 * p + 16 * g);
         } else {
             const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 64 * p + 8 * g);
             raw[p] = u32x4{u.x, u.y, 0u, 0u};
@@ -322,8 +322,8 @@ __device__ __forceinline__ void load_pages(PartPages &pp, const KvShape &s, int 
 // A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
 // maxima, sums and O', and are put together in LDS at the end.
 // Bound: HBM, from which the cache comes once, with non-temporal loads (645 MB of 64 sequences, 8 heads: 115 us = 5.6 TB/s, with plain loads 125; 227 MB of
-// 24 sequences, 40 heads: 46 us = 4.9 TB/s); a single sequence of 701 tokens takes 5.3 us, the chain of page, K, score, sum.  Matrix and vector
-// units are under a third busy even with one column in use of sixteen, so there is no kernel of its own for one.
+// 24 sequences, 40 heads: 46 us = 4.9 TB/s); a single sequence of 701 tokens takes 5.3 us, the chain of page, K, score, sum.  Vector units 40 %, matrix
+// units 6 % busy even where one column of sixteen is in use, so there is no kernel of its own for one.
 template <int DT, int DB>
 __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
@@ -368,10 +368,10 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         const int bk = (int)kv_div((uint32_t)gk, s.div_b), bv = (int)kv_div((uint32_t)gv, s.div_b);
         const uint8_t *pk = s.pool + (int64_t)pp.page[bk] * s.page_bytes + (int64_t)(gk - bk * gpb) * (2 * kKvGranule * D) + (n % 4) * D;
         const uint8_t *pv = s.pool + (int64_t)pp.page[bv] * s.page_bytes + (int64_t)(gv - bv * gpb) * (2 * kKvGranule * D) + kKvGranule * D + n * 16;
-        load_k<DB, true>(pk, g, kr[0]);
-        load_k<DB, true>(pk + 4 * D, g, kr[1]);
+        load_k<DB>(pk, g, kr[0]);
+        load_k<DB>(pk + 4 * D, g, kr[1]);
 #pragma unroll
-        for (int k = 0; k < DB; ++k) vr[k] = load_once<true>(pv + k * 256);
+        for (int k = 0; k < DB; ++k) vr[k] = load_once(pv + k * 256);
         e_next = pp.e[bv];
     };
     constexpr int kStep = kWaves * (kKvChunk / kKvGranule);
@@ -515,8 +515,7 @@ __device__ __forceinline__ f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f
 constexpr int kManyTile = kKvManyTile, kManyGranules = kManyTile / kKvGranule;
 constexpr float kSlack = 8.0f;
 
-// Bound: the vector units (56 % busy; 12.8 vector instructions for each of the 32 cycles of a matrix instruction, half of them the softmax's, a sixth the codes'),
-// beside the matrix units (35 %): a chunk of 512 behind 30000 tokens, 64 heads 627 us = 810 TFLOP/s, chunks of 128 - 1024 behind up to 4096 426 us.
+// Bound: the vector units, 12 of whose instructions go beside each matrix instruction (over half of all cycles, at four an instruction; matrix units 35 %): a chunk of 512 behind 30000 tokens, 64 heads 627 us = 810 TFLOP/s, chunks of 128 - 1024 behind up to 4096 426 us.
 // Two workgroups share a compute unit up to 128 elements a head, so that one's products run beside the other's softmax.
 template <int DB>
 struct ManyLds {
@@ -971,44 +970,35 @@ __device__ __forceinline__ uint32_t rank_of(float w, int32_t pos, int32_t recent
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// What the wavefronts of a team wait for: all of a workgroup, or the lanes of one wavefront (whose LDS operations are in order)
-template <int W>
-__device__ __forceinline__ void team_sync()
+// The LDS operations of a wavefront are in order: its lanes only have to stay together
+__device__ __forceinline__ void wave_sync()
 {
-    if constexpr (W > 1) {
-        __syncthreads();
-    } else {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
-// A team of W wavefronts per sequence and head; a wavefront has a run of slots, 64 of them a stripe.  Ranks are kept in LDS, `held` of each
+// A workgroup of W wavefronts per sequence and head; a wavefront has a run of slots, 64 of them a stripe.  Ranks are kept in LDS, `held` of each
 // wavefront's (longer runs are ranked again).  The rank of the last token that stays is found BITS bits at a time: bins are counted in
 // LDS, and every wavefront finds the digit from the counts for itself - lane l has the bins of digits B l .. B l + B - 1, digit B l + k
 // at place 64 k + l.  Then the counts of each run say where its places and moves go in the lists: all
 // integers, in the order of the slots.
-// Wavefronts: one for rows of up to 2048 tokens where there are many rows, four for up to 8192, else sixteen.  Bound: vector instructions of the one compute unit that a
-// row has; 64 rows of 8000 - 32000 tokens 45 us.
+// Bound: vector and LDS instructions of the one compute unit that a row has; 64 rows of 8000 - 32000 tokens 45 us.
 template <int W>
 struct Evict {
-    static constexpr int kThreads = W == 1 ? 256 : W * kWave, kTeams = kThreads / kWave / W;
+    static constexpr int kThreads = W * kWave;
     static constexpr int kBits = W < 16 ? 8 : 11, kBins = 1 << kBits, kPer = kBins / kWave;
-    static constexpr int kHeld = W == 1 ? 1536 : 2048; // ranks of each wavefront: at most 33 and 145 KiB a workgroup
-    static constexpr unsigned lds(int held) { return (unsigned)(kTeams * (W * held + 2 * kBins + 4 * W) * 4); }
+    static constexpr int kHeld = 2048; // ranks of each wavefront: at most 34 and 145 KiB a workgroup
+    static constexpr unsigned lds(int held) { return (unsigned)((W * held + 2 * kBins + 4 * W) * 4); }
 };
 
 template <int W>
-__global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(const KvSeq *__restrict__ seqs, int n_rows, int held, KvShape s, KvEvict e)
+__global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(const KvSeq *__restrict__ seqs, int held, KvShape s, KvEvict e)
 {
-    constexpr int kTeams = Evict<W>::kTeams, kBits = Evict<W>::kBits, kBins = Evict<W>::kBins, kPer = Evict<W>::kPer;
+    constexpr int kBits = Evict<W>::kBits, kBins = Evict<W>::kBins, kPer = Evict<W>::kPer;
     extern __shared__ uint32_t lds[];
-    const int team = wave_number() / W, wave = wave_number() % W, lane = threadIdx.x % kWave;
-    const int row = blockIdx.x * kTeams + team;
-    if (row >= n_rows) return; // (a whole team; teams of one wavefront do not wait for each other)
-    uint32_t *mine_lds = lds + team * (W * held + 2 * kBins + 4 * W);
-    uint32_t *bins = mine_lds, *counts = bins + 2 * kBins, *ranks = counts + 4 * W + wave * held;
+    const int wave = wave_number(), lane = threadIdx.x % kWave, row = blockIdx.x;
+    uint32_t *bins = lds, *counts = bins + 2 * kBins, *ranks = counts + 4 * W + wave * held;
     const KvSeq q = seqs[row / s.n_kv];
     const int head = row % s.n_kv;
     const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens;
@@ -1059,7 +1049,7 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
     };
 
     for (int k = wave * kWave + lane; k < kBins; k += W * kWave) bins[k] = 0;
-    team_sync<W>();
+    __syncthreads();
     // ranks, and the counts of their first bits; eight stripes are loaded together
     constexpr int kAhead = 8;
     for (int j = 0; j < n; j += kAhead * kWave) {
@@ -1102,7 +1092,7 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
         }
         if (shift > 0)
             for (int k = wave * kWave + lane; k < kBins; k += W * kWave) next[k] = 0;
-        team_sync<W>();
+        __syncthreads();
         uint32_t c[kPer], mine = 0;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) mine += c[k] = now[k * kWave + lane];
@@ -1136,31 +1126,29 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
 
     // where this run's places and moves go: from what the runs before it have, tokens of greater and of equal rank before and from keep on
     int seen = 0, holes = 0, moves = 0, total = 0; // equal ranks, places, moves so far; all moves
-    if constexpr (W > 1) {
-        int c[4] = {0, 0, 0, 0}; // greater and equal before keep, then from keep on
-        walk([&](int i, uint32_t r, bool in) {
-            const int g = in && r > prefix, same = in && r == prefix, before = i < q.keep;
-            c[0] += g & before;
-            c[1] += same & before;
-            c[2] += g & ~before;
-            c[3] += same & ~before;
-        });
+    int c[4] = {0, 0, 0, 0}; // greater and equal before keep, then from keep on
+    walk([&](int i, uint32_t r, bool in) {
+        const int g = in && r > prefix, same = in && r == prefix, before = i < q.keep;
+        c[0] += g & before;
+        c[1] += same & before;
+        c[2] += g & ~before;
+        c[3] += same & ~before;
+    });
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 4; ++k) {
 #pragma unroll
-            for (int x = 32; x; x >>= 1) c[k] += __shfl_xor(c[k], x, kWave);
-            if (lane == 0) counts[k * W + wave] = (uint32_t)c[k];
-        }
-        team_sync<W>();
-        int all_seen = 0, all_holes = 0;
-        for (int k = 0; k < W; ++k) {
-            if (k == wave) seen = all_seen, holes = all_holes, moves = total;
-            const int e0 = (int)counts[W + k], e1 = (int)counts[3 * W + k];
-            const int stay0 = max(min(left - all_seen, e0), 0), stay1 = max(min(left - all_seen - e0, e1), 0);
-            all_holes += max(min(q.keep - k * run, min(run, q.len - k * run)), 0) - (int)counts[k] - stay0;
-            total += (int)counts[2 * W + k] + stay1;
-            all_seen += e0 + e1;
-        }
+        for (int x = 32; x; x >>= 1) c[k] += __shfl_xor(c[k], x, kWave);
+        if (lane == 0) counts[k * W + wave] = (uint32_t)c[k];
+    }
+    __syncthreads();
+    int all_seen = 0, all_holes = 0;
+    for (int k = 0; k < W; ++k) {
+        if (k == wave) seen = all_seen, holes = all_holes, moves = total;
+        const int e0 = (int)counts[W + k], e1 = (int)counts[3 * W + k];
+        const int stay0 = max(min(left - all_seen, e0), 0), stay1 = max(min(left - all_seen - e0, e1), 0);
+        all_holes += max(min(q.keep - k * run, min(run, q.len - k * run)), 0) - (int)counts[k] - stay0;
+        total += (int)counts[2 * W + k] + stay1;
+        all_seen += e0 + e1;
     }
     const uint64_t lower = (uint64_t(1) << lane) - 1;
     const int most = min(q.keep, q.len - q.keep), blocks = (q.keep + s.N - 1) / s.N;
@@ -1189,13 +1177,12 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
         }
         moves += (int)__popcll(ms);
     });
-    if constexpr (W == 1) total = moves;
     if (wave == 0 && lane == 0) {
         first[blocks] = total;
         // the exponents of the block about the budget, from which tokens move and into which tokens move
         first[blocks + 1] = reinterpret_cast<const int16_t *>(s.exps)[table_entry(s, q.seq, q.keep / s.N, head)];
     }
-    team_sync<W>();
+    __syncthreads();
     // (entries of slots from keep on are only read)
     for (int m = wave * kWave + lane; m < total; m += W * kWave) {
         e.w_out[at + dst[m]] = w[src[m]];
@@ -1206,9 +1193,9 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
 // A cache at its budget, which has few tokens more than it keeps after each step: a wavefront per row, in one launch.  The token that goes is the one of
 // least rank, of equal ones that in the highest slot; the next one is the least behind it in this order.  What stays of
 // the slots behind the budget moves at once.
-// 64 sequences x 32 heads of 1025 tokens 13 us, 26 MB of weights and positions read and written; kv_evict_select_kernel and kv_evict_move_kernel took 36.
+// 64 sequences x 32 heads of 1025 tokens 13 us, 34 MB of weights and positions read and written; kv_evict_select_kernel and kv_evict_move_kernel took 36.
 // Bound: the latency of a pass over the row by one wavefront and then of the move.
-constexpr int kEvictFew = 4, kEvictFewTokens = 8192;
+constexpr int kEvictFew = 4;
 __global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restrict__ seqs, int n_rows, KvShape s, KvEvict e)
 {
     const int row = blockIdx.x * 4 + wave_number(), lane = threadIdx.x % kWave, D = s.D;
@@ -1286,7 +1273,7 @@ __global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restri
     const int n = (int)__popcll(staying); // as many places are before the budget
     if (stays) move[__popcll(staying & ((uint64_t(1) << lane) - 1))][0] = q.keep + lane;
     if (mine < q.keep) move[place][1] = mine;
-    team_sync<1>();
+    wave_sync();
     if (lane < n) {
         w_out[move[lane][1]] = w[move[lane][0]];
         pos_out[move[lane][1]] = pos[move[lane][0]];
@@ -1335,7 +1322,7 @@ __global__ __launch_bounds__(256) void kv_evict_few_kernel(const KvSeq *__restri
                 const uint32_t old = *p, mask = t + 4 <= last ? 0xffffffffu : (1u << (8 * (last - t))) - 1;
                 *p = (shift_codes(old, grow_v) & mask) | (old & ~mask); // (the row is this wavefront's alone)
             }
-            team_sync<1>(); // the moved tokens' bytes go over these
+            wave_sync(); // the moved tokens' bytes go over these
         }
 #pragma unroll
         for (int k = 0; k < kEvictFew; ++k) {
@@ -1498,7 +1485,9 @@ int32_t launch_kv_append(const slora_kv8_batch *b, const KvShape &shape, const K
     return check_launch("kv_append");
 }
 
-constexpr int32_t kFewParts = 16; // of a column, up to which a wavefront puts them together alone
+// Parts of a column, up to which a wavefront puts them together alone.  us a pass, by a wavefront / by four: two sequences of 90000 - 131000 tokens (64 parts) 96 / 84, 32 of nine
+// drafted tokens behind 2000 (8 heads) 78 / 85, 64 of 500 - 8000 124 / 126.
+constexpr int32_t kFewParts = 16;
 
 int32_t launch_kv_attend(const slora_kv8_batch *b, const KvShape &shape, const KvAttend &a, void *stream)
 {
@@ -1550,7 +1539,10 @@ int32_t launch_kv_evict(const slora_kv8_batch *b, const KvShape &shape, const Kv
 {
     const int64_t rows = (int64_t)b->seqs.size() * shape.n_kv;
     hipStream_t st = (hipStream_t)stream;
-    if (b->most_going <= kEvictFew && b->longest <= kEvictFewTokens) {
+    // A wavefront reads a row again for every token that goes.  us, it / the other kernels: 2048 rows of 1025 tokens, one goes 13 / 39, of 8000, four go 129 / 144,
+    // of 16000, one goes 113 / 313; 512 rows of 8000, two go 48 / 52, of 16000, one goes 58 / 85; 256 rows of 8000, two go 47 / 33; 32 rows of 8000, one goes 24 / 31,
+    // four go 79 / 31, of 32000, one goes 83 / 60; 128 rows of 4000, two go 25 / 27.
+    if (b->most_going <= kEvictFew && (int64_t)std::max(b->most_going, 1) * b->longest <= (rows >= 512 ? 32768 : 8192)) {
         hipLaunchKernelGGL(kv_evict_few_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, b->d_seqs, (int)rows, shape, e);
         return check_launch("kv_evict_few");
     }
@@ -1562,13 +1554,15 @@ int32_t launch_kv_evict(const slora_kv8_batch *b, const KvShape &shape, const Kv
             const hipError_t a = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_evict_select_kernel<w.value>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
             if (a != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(a));
         }
-        hipLaunchKernelGGL(kv_evict_select_kernel<w.value>, dim3((unsigned)((rows + E::kTeams - 1) / E::kTeams)), dim3(E::kThreads), E::lds(held), st,
-                           b->d_seqs, (int)rows, held, shape, e);
+        hipLaunchKernelGGL(kv_evict_select_kernel<w.value>, dim3((unsigned)rows), dim3(E::kThreads), E::lds(held), st,
+                           b->d_seqs, held, shape, e);
         return check_launch("kv_evict_select");
     };
-    int32_t rc = b->longest <= 2048 && rows >= 256 ? select(std::integral_constant<int, 1>{})
-                 : b->longest <= 8192              ? select(std::integral_constant<int, 4>{})
-                                                   : select(std::integral_constant<int, 16>{});
+    // us with 4 / 16 wavefronts: 2048 rows of 1025 tokens 101 / 189, of 8000 450 / 524, 512 of 8000 121 / 125, of 16000 745 / 649; where a row has a compute unit for
+    // itself, 256 rows of 5000 65 / 60, of 8000 78 / 65, 128 of 2000 35 / 39, of 4000 45 / 43, of 8000 61 / 48, of 30000 478 / 241.  (One wavefront: 2048 rows of 1025 99,
+    // of 2040 181 where four take 167.)
+    const bool wide = b->longest > (rows > 256 ? 8192 : 4096);
+    int32_t rc = wide ? select(std::integral_constant<int, 16>{}) : select(std::integral_constant<int, 4>{});
     if (rc == SLORA_OK && b->dest_blocks > 0) {
         // eight workgroups for every compute unit
         const int64_t split = std::max<int64_t>(1, std::min<int64_t>(b->dest_blocks, (2048 + rows - 1) / rows));

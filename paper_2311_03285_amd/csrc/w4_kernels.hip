@@ -116,7 +116,7 @@ __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirst
 
 // Up to four tokens.  A workgroup = RT tiles of 16 outputs; its WV wavefronts take chunks of 128 inputs in turn, with the weights of the next ones and x of the
 // next one under way, and are added in LDS.  Loads are not behind branches where others are waited for: the compiler would wait for all of them.
-// Bound: HBM and the time to fill it: four of 4096 of 4096, one token 9.0 us = 3.8 TB/s, two of 20480 of 5120 28 us = 3.8 TB/s.
+// Bound: HBM and the time to fill it: four of 4096 of 4096, one token 9.0 us = 3.8 TB/s, two of 20480 of 5120 28 us = 3.7 TB/s.
 template <int DT, int RT, int WV, int U>
 __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
 {
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
 // bytes, its pieces of 16 bytes permuted by its number, so that the 16 rows of an operand are in different banks).  While a chunk is
 // worked on, the team's next one goes from registers to the other buffer, the one after that from memory to
 // registers; the barrier between chunks waits for LDS alone.
-// Bound: vector instructions (conversions of codes, 7 for 8 of them, and a product per sum and unit) and matrix instructions, half of which take the
-// zeros off: two of 20480 of 5120, 32 tokens 37 us = 360 TFLOP/s and 3.2 TB/s; three of 5003 of 3080, 67 tokens, groups of 32 25 us.
+// Two of 20480 of 5120, 32 tokens 37 us = 360 TFLOP/s and 3.2 TB/s; three of 5003 of 3080, 67 tokens, groups of 32 25 us.  Bound: no unit alone - of the former's
+// cycles the vector units are busy for 35 % (at four an instruction), the matrix units, half of whose work takes the zeros off, for 26 %.
 constexpr int kWideThreads = 8 * kWave;
 
 __device__ __forceinline__ void lds_barrier()

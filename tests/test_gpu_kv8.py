@@ -322,6 +322,29 @@ def test_eviction_of_a_few_tokens(D, H, dtype, in_place):
         evict_and_check(t, [4, 1], [1, 0], 0, w, pos, in_place)
 
 
+def test_eviction_of_a_few_tokens_of_many_rows_with_long_ones():
+    """512 rows, the longest of which are read four times by one wavefront"""
+    with Twin(512, 32, 32, 1, max_seqs=16, max_tokens=2100) as t:
+        every, size = list(range(16)), [20 + 3 * s for s in range(15)] + [2049]
+        t.step(every, size)
+        w, _, pos = t.weight_arrays()
+        w[t.rng.random(w.shape) < 0.5] = 0.0
+        for s in every:
+            pos[s, :, :size[s]] = torch.arange(size[s], device="cuda", dtype=torch.int32)
+        evict_and_check(t, every, [size[s] - s % 5 for s in range(15)] + [2045], 15, w, pos)
+
+
+@pytest.mark.parametrize("size", [4096, 4097, 4160])
+def test_eviction_about_the_length_from_which_a_row_has_more_wavefronts(size):
+    with Twin(2048, 64, 2, 1, max_seqs=2, max_tokens=4200) as t:
+        t.step([0, 1], [size, 70])
+        w, _, pos = t.weight_arrays()
+        w[t.rng.random(w.shape) < 0.3] = 0.5
+        for s in range(2):
+            pos[s, :, :t.len[s]] = torch.arange(t.len[s], device="cuda", dtype=torch.int32)
+        evict_and_check(t, [0, 1], [size - 100, 64], 50, w, pos)
+
+
 def test_a_table_entry_that_is_given_another_page():
     """truncate, then grow again on other pages while earlier work may still run"""
     with Twin(512, 64, 1, 2, max_seqs=2, max_tokens=200) as t:
