@@ -18,6 +18,12 @@ constexpr int kKvManyCols = 128, kKvManyThreads = 256; // columns of a workgroup
 constexpr int kKvManyFrom = 33;
 constexpr int kKvPartBlocks = 512;   // most blocks of a part of a sequence: their page numbers are held in LDS
 
+// Arrays of bins that an eviction's digits are counted in.  With one barrier a turn, the wavefronts count into array a before it and read a behind it,
+// and clear the array of the next turn before it: that one was last read behind the barrier before the last, so it has to be neither a nor
+// the array before a, which a slow wavefront may still be reading.
+constexpr int kKvBinArrays = 3;
+constexpr int kv_next_bins(int a) { return a + 1 == kKvBinArrays ? 0 : a + 1; }
+
 // a sequence of the batch
 struct KvSeq {
     int32_t seq, len;  // its number, tokens it holds

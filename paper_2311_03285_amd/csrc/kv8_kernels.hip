@@ -988,8 +988,8 @@ template <int W>
 struct Evict {
     static constexpr int kThreads = W * kWave;
     static constexpr int kBits = W < 16 ? 8 : 11, kBins = 1 << kBits, kPer = kBins / kWave;
-    static constexpr int kHeld = 2048; // ranks of each wavefront: at most 34 and 145 KiB a workgroup
-    static constexpr unsigned lds(int held) { return (unsigned)((W * held + 2 * kBins + 4 * W) * 4); }
+    static constexpr int kHeld = 2048; // ranks of each wavefront: at most 35 and 153 KiB a workgroup
+    static constexpr unsigned lds(int held) { return (unsigned)((W * held + kKvBinArrays * kBins + 4 * W) * 4); }
 };
 
 template <int W>
@@ -998,7 +998,7 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
     constexpr int kBits = Evict<W>::kBits, kBins = Evict<W>::kBins, kPer = Evict<W>::kPer;
     extern __shared__ uint32_t lds[];
     const int wave = wave_number(), lane = threadIdx.x % kWave, row = blockIdx.x;
-    uint32_t *bins = lds, *counts = bins + 2 * kBins, *ranks = counts + 4 * W + wave * held;
+    uint32_t *bins = lds, *counts = bins + kKvBinArrays * kBins, *ranks = counts + 4 * W + wave * held;
     const KvSeq q = seqs[row / s.n_kv];
     const int head = row % s.n_kv;
     const int64_t at = ((int64_t)q.seq * s.n_kv + head) * s.max_tokens;
@@ -1081,11 +1081,11 @@ __global__ __launch_bounds__(Evict<W>::kThreads) void kv_evict_select_kernel(con
     // the rank of the keep-th token, and how many of that rank stay
     uint32_t prefix = 0;
     int left = q.keep;
-    int turn = 0;
+    int array = 0;
 #pragma unroll 1
-    for (int top = 32; top > 0; top -= kBits, turn ^= 1) {
+    for (int top = 32; top > 0; top -= kBits, array = kv_next_bins(array)) {
         const int shift = max(top - kBits, 0);
-        uint32_t *now = bins + turn * kBins, *next = bins + (turn ^ 1) * kBins;
+        uint32_t *now = bins + array * kBins, *next = bins + kv_next_bins(array) * kBins;
         if (top < 32) {
             const uint32_t mask = (1u << (top - shift)) - 1;
             walk([&](int, uint32_t r, bool in) { count(now, (r >> shift) & mask, in && (r >> top) == (prefix >> top)); });
