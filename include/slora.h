@@ -460,6 +460,7 @@ int32_t slora_kv8_append(slora_kv8_batch *batch, int32_t layer, const void *k, i
  * weights_in, weights_out, pos: NULL, or DEVICE arrays [max_seqs][n_kv_heads][max_tokens] of this layer:
  *   weights_out[j] = weights_in[j] (0 for the batch's own tokens) + sum of p_j over the sequence's rows and the heads that share j's head,
  *   in fp32; pos[j] = position of j, written for the batch's own tokens.
+ *   p is of scores alone: an infinity or NaN in V spoils outputs and no weight.
  * weights_in may be weights_out.  Only entries of the sequences' tokens are touched.  Results do not depend on
  * what else runs: no floating-point atomics, one order per batch.
  */

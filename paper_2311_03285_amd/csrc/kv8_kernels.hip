@@ -392,7 +392,9 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         const int bound = min(limit, g1 * kKvGranule) - token; // tokens of this lane's granule that its column sees
         if constexpr (more.value) fetch(gr + kStep);
 
-        const float f = unit * unit_of(ek), add = ev == kKvPoison ? __uint_as_float(0x7fc00000u) : (float)ev;
+        // (an infinity or NaN in V spoils what the column adds up of V, not its scores' sum, which the weights are taken from)
+        const bool spoiled = ev == kKvPoison;
+        const float f = unit * unit_of(ek), add = spoiled ? 0.0f : (float)ev;
         float t[8], top = -INFINITY;
         if (a.scores && q.score0 >= 0) {
             float *at = a.scores + (q.score0 + ((int64_t)head * (q.rows * s.G) + col) * (int64_t)((q.len + 7) / 8 * 8)) + token;
@@ -425,7 +427,11 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
             sum += x;
             p[i] = (_Float16)x;
         }
-        l = __builtin_fmaf(l, keep, bound > 0 ? sum * unit_of(-ev) : 0.0f);
+        if (__any(spoiled)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = spoiled && i < bound ? (_Float16)__uint_as_float(0x7fc00000u) : p[i];
+        }
+        l = __builtin_fmaf(l, keep, bound > 0 ? sum * (spoiled ? 1.0f : unit_of(-ev)) : 0.0f);
         if (__any(keep != 1.0f)) {
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) o[k] *= keep;
@@ -521,7 +527,8 @@ template <int DB>
 struct ManyLds {
     static constexpr int kUnits = kManyTile * DB * 4; // of 16 bytes, K's or V's of a tile
     u32x4 k[2][kUnits], v[2][kUnits];
-    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, ev, 2^-ev of each granule
+    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, ev, 2^-ev of each granule; 0 and 1 for a V with an infinity or NaN,
+    uint32_t spoiled[2];                                                          // the granules of which this has the bits of
     PartPages pages;
 };
 
@@ -594,8 +601,10 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
             const int gk = min(g + (int)threadIdx.x, g1 - 1) - base, e = lds.pages.e[kv_div((uint32_t)gk, s.div_b)];
             const int ek = (int8_t)(e & 0xff), ev = e >> 8;
             lds.unit[buffer][threadIdx.x] = unit_of(ek);
-            lds.add[buffer][threadIdx.x] = ev == kKvPoison ? __uint_as_float(0x7fc00000u) : (float)ev;
-            lds.less[buffer][threadIdx.x] = unit_of(-ev);
+            lds.add[buffer][threadIdx.x] = ev == kKvPoison ? 0.0f : (float)ev;
+            lds.less[buffer][threadIdx.x] = ev == kKvPoison ? 1.0f : unit_of(-ev);
+            const uint64_t spoiled = __ballot(ev == kKvPoison);
+            if (threadIdx.x == 0) lds.spoiled[buffer] = (uint32_t)spoiled;
         }
     };
     // this lane's token in row n of a half of the tile, and its place in LDS for units 2 s + h, s even and odd
@@ -691,6 +700,17 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
                     }
                     l = __builtin_fmaf(sum, lds.less[buffer][4 * t + 2 * r + h], l);
                 }
+            // an infinity or NaN in V spoils what the columns that see it add up of V, not their scores' sum, which the weights are taken from
+            if (const uint32_t spoiled = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds.spoiled[buffer])) {
+                const int bound = min(limit, g1 * kKvGranule) - first - 8 * h;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if ((spoiled >> (4 * t + 2 * r + h) & 1) && t * 32 + r * 16 + i < bound) p[t][r][i] = (_Float16)__uint_as_float(0x7fc00000u);
+            }
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll

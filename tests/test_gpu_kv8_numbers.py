@@ -1,0 +1,53 @@
+"""Numbers that attention over the 8-bit cache may meet and that a mean over tokens hides: infinities and NaN in parts of a cache, weights beside
+them, ranges far apart.  Against the oracle in 64 bits with its bounds; NaN has to be where the definition has it, and nowhere else."""
+import numpy as np
+import pytest
+import torch
+
+from kv8_util import Twin
+from oracle import np_kv8
+from paper_2311_03285_amd import slora
+
+pytestmark = pytest.mark.gpu
+
+# new tokens of a sequence, heads that share one of the cache: weights from kept scores, weights from K again behind either form of attention
+PATHS = [(5, 2), (12, 2), (40, 2)]
+
+
+def check_weights(t, seqs, counts, before, after):
+    """after = before + what the oracle says the tokens drew, NaN where that is NaN"""
+    for s, n in zip(seqs, counts):
+        size = t.len[s]
+        for h in range(t.kv):
+            total, slack = t.drawn[s, h]
+            ref = total.copy()
+            old = max(size - n, 0)
+            ref[:old] += before[s, h, :old]
+            got = after[s, h, :size]
+            assert np.array_equal(np.isnan(got), np.isnan(ref)), (s, h, np.nonzero(np.isnan(got) != np.isnan(ref))[0])
+            ok = ~np.isnan(ref)
+            assert (np.abs(got - ref)[ok] <= (slack + np.abs(ref) * 2.0 ** -22)[ok]).all(), (s, h)
+            assert np.array_equal(after[s, h, size:], np.full(t.max_tokens - size, -1.0, np.float32))
+
+
+def attend_with_weights(t, batch, seqs, counts, **kw):
+    w_in, w_out, pos = t.weight_arrays()
+    out, q = t.attend(batch, 0, seqs, counts, weights=(w_in, w_out, pos), **kw)
+    check_weights(t, seqs, counts, w_in.cpu().numpy(), w_out.cpu().numpy())
+    return out, q
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,G", PATHS)
+def test_a_bad_v_spoils_outputs_and_no_weight(n, G, dtype):
+    """the weights are of scores alone, whatever V holds"""
+    with Twin(512, 32, 2, G, dtype, max_seqs=2, max_tokens=200) as t:
+        rows = t.rows(100 + 33)
+        rows[20, 1, 0, 3] = float("inf")  # sequence 0, head 0, an old token
+        t.step([0, 1], [100, 33], rows=rows)
+        new = t.rows(2 * n)
+        new[n + n // 2, 1, 1, 9] = float("nan")  # sequence 1, head 1, a new token: earlier rows that do not see its block stay numbers
+        batch = t.step([0, 1], [n, n], rows=new)
+        out, _ = attend_with_weights(t, batch, [0, 1], [n, n])
+        nan = torch.isnan(out)
+        assert nan[:n, :G * 32].all() and not nan[:n, G * 32:].any() and not nan[n:, :G * 32].any() and nan[2 * n - 1, G * 32:].all()
