@@ -948,15 +948,20 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const KvSeq *__restrict
         for (int j = 0; j < kSteps; ++j) sc = mfma32(kf[j], __builtin_bit_cast(f16x8, lds.q[buffer][(2 * j + h) * 32 + (n ^ turn(2 * j + h))]), sc);
         const float unit = lds.unit[buffer][n], m = lds.m[buffer][n], by = lds.by[buffer][n];
         const int limit = lds.limit[buffer][n];
-        const bool all_seen = __all(limit >= token0 + 32 || by == 0.0f);
+        // (what a column does not see is left out, not multiplied by 0: its score may be anything, and its sum may be NaN)
+        auto add = [&](auto all) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * k + i], unit * f[k], -m));
-                if (!all_seen) p = token0 + 8 * k + 4 * h + i < limit ? p : 0.0f;
-                w[4 * k + i] = __builtin_fmaf(p, by, w[4 * k + i]);
-            }
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * k + i], unit * f[k], -m)), sum = __builtin_fmaf(p, by, w[4 * k + i]);
+                    w[4 * k + i] = all.value || token0 + 8 * k + 4 * h + i < limit ? sum : w[4 * k + i];
+                }
+        };
+        if (__all(limit >= token0 + 32))
+            add(std::true_type{});
+        else
+            add(std::false_type{});
         if (c0 + 32 < cols) put(buffer ^ 1);
         __syncthreads();
     }
