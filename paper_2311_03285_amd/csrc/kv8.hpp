@@ -69,8 +69,8 @@ struct KvAttend {
     int64_t q_stride, out_stride;
     float scale;    // times log2(e)
     int32_t causal;
-    float *part_o;  // sums of parts: [column][head][D]
-    float *part_ml; // ... [column][head] {maximum, sum}
+    float *part_o;  // averages of V of parts: [column][head][D]
+    float *part_ml; // ... [column][head] {m, l}: their scores' sums l * 2^m
     float *stat;    // [row][query head] {maximum, 1 / sum}
     float *scores;  // see KvSeq; NULL: not wanted
 };

@@ -209,8 +209,12 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
 // into operands.  Codes become binary16 exactly (|c| <= 127); q in bfloat16 is scaled by a power of two of its own into the range of
 // binary16, which keeps its eight bits down to 2^-28 of the row's largest.
 //
-// Softmax: with scores s (times log2 e) and V's exponents ev, the running maximum is of s + ev, so that
-// p = 2^(s + ev - m) <= 1 is what the second product needs of V's units, as a binary16 number; the sum that divides takes p * 2^-ev.
+// Softmax: with scores s (times log2 e) and V's exponents ev, u = max(ev - top, -100) for the largest exponent `top` of the part, the
+// running maximum is of s + u, so that p = 2^(s + u - m) <= 1 is what the second product needs of V's units, as a binary16 number; the sum that
+// divides takes p * 2^-u.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
+// p >= 2^-100.  V of a block further below `top` is read in units of 2^(top - 100) instead of its own, which puts its elements off by less than 2^(top - 93).
+// A block with an infinity or NaN in V has u = 0, and the columns that see any of its tokens - their limits are behind its first one - get NaN at the end: the
+// scores' sum, which the weights are taken from, knows nothing of V.
 __device__ __forceinline__ f32x4 mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // four codes -> binary16: 0x6400 | u is 1024 + u for a byte u; c + 128 = u
@@ -305,6 +309,34 @@ __device__ __forceinline__ f16x8 k_operand(const u32x4 (&raw)[(DB + 1) / 2], int
     return j % 2 ? codes_to_f16x8(raw[j / 2].z, raw[j / 2].w) : codes_to_f16x8(raw[j / 2].x, raw[j / 2].y);
 }
 
+constexpr int kKvFar = 100; // see above
+
+// the largest of the lanes' numbers, without LDS: rows of 16, then what the rows before have found
+__device__ __forceinline__ int wave_max(int v)
+{
+#define SLORA_STEP(control) v = max(v, __builtin_amdgcn_update_dpp(v, v, control, 0xf, 0xf, false))
+    SLORA_STEP(0x111); // row_shr 1, 2, 4, 8
+    SLORA_STEP(0x112);
+    SLORA_STEP(0x114);
+    SLORA_STEP(0x118);
+    SLORA_STEP(0x142); // row_bcast 15, 31
+    SLORA_STEP(0x143);
+#undef SLORA_STEP
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// what a part's exponents of V are taken against
+struct Units {
+    int top;     // the largest of them
+    int spoiled; // the first block of the part that holds an infinity or NaN, if any
+    __device__ __forceinline__ int of(int ev) const { return ev == kKvPoison ? 0 : max(ev - top, -kKvFar); }
+    // what a column's sums of p V are multiplied by (limit: tokens that it sees; a block's first token: N of them before each)
+    __device__ __forceinline__ float scale(float by, int limit, int N, int block0) const
+    {
+        return spoiled < INT32_MAX && limit > (block0 + spoiled) * N ? __uint_as_float(0x7fc00000u) : by * unit_of(top);
+    }
+};
+
 // Pages and exponents of the blocks of a part, in LDS
 struct PartPages {
     int32_t page[kKvPartBlocks];
@@ -317,6 +349,28 @@ __device__ __forceinline__ void load_pages(PartPages &pp, const KvShape &s, int 
         pp.page[i] = s.table[entry];
         pp.e[i] = reinterpret_cast<const int16_t *>(s.exps)[entry];
     }
+}
+// (every wavefront for itself, behind the barrier that ends load_pages)
+__device__ __forceinline__ Units units_of(const PartPages &pp, int blocks)
+{
+    const int lane = threadIdx.x % kWave;
+    int top = kKvLowest, spoiled = INT32_MAX;
+    for (int i0 = 0; i0 < blocks; i0 += kWave) {
+        const int ev = i0 + lane < blocks ? pp.e[i0 + lane] >> 8 : kKvLowest;
+        const uint64_t bad = __ballot(ev == kKvPoison);
+        if (bad) spoiled = min(spoiled, i0 + (int)__ffsll((unsigned long long)bad) - 1);
+        top = max(top, ev == kKvPoison ? kKvLowest : ev);
+    }
+    return {wave_max(top), spoiled};
+}
+
+// A part leaves its own average of V, whose units are its own, and {m, l}, its scores' sum as l * 2^m: l below 2^65 keeps l * 2^(m - the largest m) a
+// normal number wherever it matters (its u may have made it 2^100 times its share).
+__device__ __forceinline__ void put_sum(float *to, float m, float l)
+{
+    const bool large = l >= 0x1p64f;
+    to[0] = large ? m + 64.0f : m;
+    to[1] = large ? l * 0x1p-64f : l;
 }
 
 // A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
@@ -346,7 +400,8 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
     const int tokens = a.causal ? min(old + last_row + 1, q.len) : q.len;
     const int g1 = min(it.d, (max(tokens, 0) + kKvGranule - 1) / kKvGranule), g0 = it.c;
     const int block0 = g0 / gpb, base = block0 * gpb;
-    if (g1 > g0) load_pages(pp, s, q.seq, head, block0, (g1 - 1) / gpb + 1 - block0);
+    const int blocks = g1 > g0 ? (g1 - 1) / gpb + 1 - block0 : 0;
+    load_pages(pp, s, q.seq, head, block0, blocks);
 
     f16x8 qf[DB];
     float unit;
@@ -355,6 +410,7 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
     unit *= a.scale;
     __syncthreads();
 
+    Units units;
     f32x4 o[2 * DB];
 #pragma unroll
     for (int k = 0; k < 2 * DB; ++k) o[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -392,9 +448,8 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         const int bound = min(limit, g1 * kKvGranule) - token; // tokens of this lane's granule that its column sees
         if constexpr (more.value) fetch(gr + kStep);
 
-        // (an infinity or NaN in V spoils what the column adds up of V, not its scores' sum, which the weights are taken from)
-        const bool spoiled = ev == kKvPoison;
-        const float f = unit * unit_of(ek), add = spoiled ? 0.0f : (float)ev;
+        const int u = units.of(ev);
+        const float f = unit * unit_of(ek), add = (float)u;
         float t[8], top = -INFINITY;
         if (a.scores && q.score0 >= 0) {
             float *at = a.scores + (q.score0 + ((int64_t)head * (q.rows * s.G) + col) * (int64_t)((q.len + 7) / 8 * 8)) + token;
@@ -427,11 +482,7 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
             sum += x;
             p[i] = (_Float16)x;
         }
-        if (__any(spoiled)) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = spoiled && i < bound ? (_Float16)__uint_as_float(0x7fc00000u) : p[i];
-        }
-        l = __builtin_fmaf(l, keep, bound > 0 ? sum * (spoiled ? 1.0f : unit_of(-ev)) : 0.0f);
+        l = __builtin_fmaf(l, keep, sum * unit_of(-u));
         if (__any(keep != 1.0f)) {
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) o[k] *= keep;
@@ -444,8 +495,9 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         }
     };
     int gr = g0 + wave * (kKvChunk / kKvGranule);
+    if (gr < g1) fetch(gr);
+    units = units_of(pp, blocks); // (while the first chunk is on its way)
     if (gr < g1) {
-        fetch(gr);
         for (; gr + kStep < g1; gr += kStep) work(gr, std::true_type{});
         work(gr, std::false_type{});
     }
@@ -479,20 +531,19 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(merge_o[k][c][d + i], x, sum[i]);
         }
+        const int r = (it.a + c) / s.G;
+        const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
+        const float scale = units.scale(by, a.causal ? min(old + r + 1, q.len) : q.len, s.N, block0);
         if (it.poff >= 0) {
             const int64_t at = (int64_t)(it.poff + c) * s.n_kv + head;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a.part_o[at * D + d + i] = sum[i];
-            if (d == 0) {
-                a.part_ml[2 * at] = top;
-                a.part_ml[2 * at + 1] = total;
-            }
+            for (int i = 0; i < 8; ++i) a.part_o[at * D + d + i] = sum[i] * scale;
+            if (d == 0) put_sum(a.part_ml + 2 * at, top, total);
         } else {
-            const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
-            const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
+            const int h = head * s.G + (it.a + c) % s.G;
             u32x4 u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = (uint32_t)narrow<DT>(sum[2 * i] * by) | ((uint32_t)narrow<DT>(sum[2 * i + 1] * by) << 16);
+            for (int i = 0; i < 4; ++i) u[i] = (uint32_t)narrow<DT>(sum[2 * i] * scale) | ((uint32_t)narrow<DT>(sum[2 * i + 1] * scale) << 16);
             *reinterpret_cast<u32x4 *>(a.out + (int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + d) = u;
             if (d == 0) {
                 float *st = a.stat + 2 * ((int64_t)(q.row0 + r) * s.n_kv * s.G + h);
@@ -527,8 +578,7 @@ template <int DB>
 struct ManyLds {
     static constexpr int kUnits = kManyTile * DB * 4; // of 16 bytes, K's or V's of a tile
     u32x4 k[2][kUnits], v[2][kUnits];
-    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, ev, 2^-ev of each granule; 0 and 1 for a V with an infinity or NaN,
-    uint32_t spoiled[2];                                                          // the granules of which this has the bits of
+    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, u, 2^-u of each granule
     PartPages pages;
 };
 
@@ -554,7 +604,8 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     const int all_see = a.causal ? min(old + (it.a + min(wave * 32, it.b - 1)) / s.G + 1, q.len) : q.len;
     const int any_sees = wave * 32 >= it.b ? 0 : a.causal ? min(old + (it.a + min(wave * 32 + 31, it.b - 1)) / s.G + 1, q.len) : q.len;
     const int block0 = g0 / gpb, base = block0 * gpb;
-    if (g1 > g0) load_pages(lds.pages, s, q.seq, head, block0, (g1 - 1) / gpb + 1 - block0);
+    const int blocks = g1 > g0 ? (g1 - 1) / gpb + 1 - block0 : 0;
+    load_pages(lds.pages, s, q.seq, head, block0, blocks);
 
     f16x8 qf[kSteps];
     float unit;
@@ -562,6 +613,8 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     load_q32<DT, DB>(real ? a.q + (int64_t)(q.row0 + row) * a.q_stride + (int64_t)qhead * D : nullptr, h, qf, unit);
     unit *= a.scale;
     __syncthreads();
+
+    const Units units = units_of(lds.pages, blocks);
 
     f32x16 o[DB];
 #pragma unroll
@@ -601,10 +654,9 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
             const int gk = min(g + (int)threadIdx.x, g1 - 1) - base, e = lds.pages.e[kv_div((uint32_t)gk, s.div_b)];
             const int ek = (int8_t)(e & 0xff), ev = e >> 8;
             lds.unit[buffer][threadIdx.x] = unit_of(ek);
-            lds.add[buffer][threadIdx.x] = ev == kKvPoison ? 0.0f : (float)ev;
-            lds.less[buffer][threadIdx.x] = ev == kKvPoison ? 1.0f : unit_of(-ev);
-            const uint64_t spoiled = __ballot(ev == kKvPoison);
-            if (threadIdx.x == 0) lds.spoiled[buffer] = (uint32_t)spoiled;
+            const int u = units.of(ev);
+            lds.add[buffer][threadIdx.x] = (float)u;
+            lds.less[buffer][threadIdx.x] = unit_of(-u);
         }
     };
     // this lane's token in row n of a half of the tile, and its place in LDS for units 2 s + h, s even and odd
@@ -700,17 +752,6 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
                     }
                     l = __builtin_fmaf(sum, lds.less[buffer][4 * t + 2 * r + h], l);
                 }
-            // an infinity or NaN in V spoils what the columns that see it add up of V, not their scores' sum, which the weights are taken from
-            if (const uint32_t spoiled = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds.spoiled[buffer])) {
-                const int bound = min(limit, g1 * kKvGranule) - first - 8 * h;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if ((spoiled >> (4 * t + 2 * r + h) & 1) && t * 32 + r * 16 + i < bound) p[t][r][i] = (_Float16)__uint_as_float(0x7fc00000u);
-            }
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -725,6 +766,11 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     l += across_32(l);
     if (!real) return;
     // elements 32 k + 8 b + 4 h + i of column n are register 4 b + i of o[k]
+    const float by = l == 0.0f ? 0.0f : 1.0f / l, scale = units.scale(by, limit, s.N, block0); // a row that sees nothing is 0
+#pragma unroll
+    for (int k = 0; k < DB; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[k][i] *= scale;
     if (it.poff >= 0) {
         const int64_t at = (int64_t)(it.poff + wave * 32 + n) * s.n_kv + head;
 #pragma unroll
@@ -732,21 +778,17 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
 #pragma unroll
             for (int b = 0; b < 4; ++b)
                 *reinterpret_cast<f32x4 *>(a.part_o + at * D + 32 * k + 8 * b + 4 * h) = f32x4{o[k][4 * b], o[k][4 * b + 1], o[k][4 * b + 2], o[k][4 * b + 3]};
-        if (h == 0) {
-            a.part_ml[2 * at] = m;
-            a.part_ml[2 * at + 1] = l;
-        }
+        if (h == 0) put_sum(a.part_ml + 2 * at, m, l);
         return;
     }
-    const float by = l == 0.0f ? 0.0f : 1.0f / l; // a row that sees nothing is 0
     uint16_t *out = a.out + (int64_t)(q.row0 + row) * a.out_stride + (int64_t)qhead * D;
 #pragma unroll
     for (int k = 0; k < DB; ++k)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
             *reinterpret_cast<u32x2 *>(out + 32 * k + 8 * b + 4 * h) =
-                u32x2{(uint32_t)narrow<DT>(o[k][4 * b] * by) | (uint32_t)narrow<DT>(o[k][4 * b + 1] * by) << 16,
-                      (uint32_t)narrow<DT>(o[k][4 * b + 2] * by) | (uint32_t)narrow<DT>(o[k][4 * b + 3] * by) << 16};
+                u32x2{(uint32_t)narrow<DT>(o[k][4 * b]) | (uint32_t)narrow<DT>(o[k][4 * b + 1]) << 16,
+                      (uint32_t)narrow<DT>(o[k][4 * b + 2]) | (uint32_t)narrow<DT>(o[k][4 * b + 3]) << 16};
     if (h == 0) {
         float *st = a.stat + 2 * ((int64_t)(q.row0 + row) * s.n_kv * s.G + qhead);
         st[0] = m == -INFINITY ? 0.0f : m;
@@ -776,20 +818,19 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__
     float total = 0.0f, sum[kPer] = {};
     constexpr int kAhead = 4;
     for (int k0 = wave; k0 < it.c; k0 += kAhead * W) {
-        float x[kAhead], l[kAhead], o[kAhead][kPer];
+        float x[kAhead], o[kAhead][kPer];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int k = k0 + j * W;
             const int64_t at = first + min(k, it.c - 1) * step;
-            x[j] = k < it.c ? __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use) : 0.0f;
-            l[j] = a.part_ml[2 * at + 1];
+            x[j] = k < it.c ? a.part_ml[2 * at + 1] * __builtin_amdgcn_exp2f(a.part_ml[2 * at] - use) : 0.0f; // its share of the scores' sum
 #pragma unroll
             for (int i = 0; i < kPer; ++i) o[j][i] = a.part_o[at * D + min(lane + 64 * i, D - 1)];
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (k0 + j * W >= it.c) break;
-            total = __builtin_fmaf(l[j], x[j], total);
+            total += x[j];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) sum[i] = __builtin_fmaf(o[j][i], x[j], sum[i]);
         }

@@ -73,3 +73,23 @@ def test_rows_that_see_nothing_draw_nothing(n):
         t.step([0, 1], [3, 20])
         batch = t.plan([0, 1], [n, n])
         attend_with_weights(t, batch, [0, 1], [n, n], size=100.0)
+
+
+@pytest.mark.parametrize("large,small", [(70, None), (100, None), (75, -50), (115, -30)])
+@pytest.mark.parametrize("old,n,G", [(60, 1, 2), (60, 5, 2), (60, 12, 2), (60, 40, 2), (3000, 1, 1), (3000, 40, 2)])
+def test_v_of_blocks_far_apart(large, small, old, n, G):
+    """blocks of V of 2^large beside blocks of zeros or of 2^small: tokens of either have their share in the scores' sum"""
+    with Twin(512, 64, 1, G, "bf16", max_seqs=1, max_tokens=3100) as t:  # blocks of 8
+        rows = t.rows(old)
+        rows[:, 1] *= 0.0 if small is None else 2.0 ** small
+        some = torch.arange(old, device="cuda") // 8 % 3 == 1
+        if old > 100:
+            some &= torch.arange(old, device="cuda") < 500  # parts that have none
+        rows[some, 1] = t.rows(int(some.sum()))[:, 1] * 2.0 ** large
+        t.step([0], [old], rows=rows)
+        new = t.rows(n)
+        new[:, 1] *= 0.0 if small is None else 2.0 ** small
+        batch = t.step([0], [n], rows=new)
+        attend_with_weights(t, batch, [0], [n])
+        if n == 1:
+            t.attend(batch, 0, [0], [n], size=6.0)
