@@ -210,8 +210,9 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
 // binary16, which keeps its eight bits down to 2^-28 of the row's largest.
 //
 // Softmax: with scores s (times log2 e) and V's exponents ev, u = max(ev - top, -100) for the largest exponent `top` of the part, the
-// running maximum is of s + u, so that p = 2^(s + u - m) <= 1 is what the second product needs of V's units, as a binary16 number; the sum that
-// divides takes p * 2^-u.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
+// running maximum is of s + u, so that p = 2^(s + u - m) <= 1 is what the second product needs of V's units; the sum that
+// divides takes p * 2^-u.  p is the one number that is rounded, to binary16.  It is taken 2^15 times as large (2^7 times for prompts, whose maximum may be 2^8 behind), the
+// largest power that stays in range, so that 11 bits are kept down to 2^-29 (2^-21) of the largest.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
 // p >= 2^-100.  V of a block further below `top` is read in units of 2^(top - 100) instead of its own, which puts its elements off by less than 2^(top - 93).
 // A block with an infinity or NaN in V has u = 0, and the columns that see any of its tokens - their limits are behind its first one - get NaN at the end: the
 // scores' sum, which the weights are taken from, knows nothing of V.
@@ -310,6 +311,7 @@ __device__ __forceinline__ f16x8 k_operand(const u32x4 (&raw)[(DB + 1) / 2], int
 }
 
 constexpr int kKvFar = 100; // see above
+constexpr int kFewUp = 15, kManyUp = 7; // powers of two of p in the second product
 
 // the largest of the lanes' numbers, without LDS: rows of 16, then what the rows before have found
 __device__ __forceinline__ int wave_max(int v)
@@ -330,10 +332,10 @@ struct Units {
     int top;     // the largest of them
     int spoiled; // the first block of the part that holds an infinity or NaN, if any
     __device__ __forceinline__ int of(int ev) const { return ev == kKvPoison ? 0 : max(ev - top, -kKvFar); }
-    // what a column's sums of p V are multiplied by (limit: tokens that it sees; a block's first token: N of them before each)
-    __device__ __forceinline__ float scale(float by, int limit, int N, int block0) const
+    // what a column's sums of 2^up p V are multiplied by (limit: tokens that it sees; a block's first token: N of them before each)
+    __device__ __forceinline__ float scale(float by, int up, int limit, int N, int block0) const
     {
-        return spoiled < INT32_MAX && limit > (block0 + spoiled) * N ? __uint_as_float(0x7fc00000u) : by * unit_of(top);
+        return spoiled < INT32_MAX && limit > (block0 + spoiled) * N ? __uint_as_float(0x7fc00000u) : by * unit_of(top - up);
     }
 };
 
@@ -478,11 +480,11 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         f16x8 p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float x = __builtin_amdgcn_exp2f(t[i] - m_use);
+            const float x = __builtin_amdgcn_exp2f(t[i] - (m_use - kFewUp));
             sum += x;
             p[i] = (_Float16)x;
         }
-        l = __builtin_fmaf(l, keep, sum * unit_of(-u));
+        l = __builtin_fmaf(l, keep, sum * unit_of(-u - kFewUp));
         if (__any(keep != 1.0f)) {
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) o[k] *= keep;
@@ -533,7 +535,7 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         }
         const int r = (it.a + c) / s.G;
         const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
-        const float scale = units.scale(by, a.causal ? min(old + r + 1, q.len) : q.len, s.N, block0);
+        const float scale = units.scale(by, kFewUp, a.causal ? min(old + r + 1, q.len) : q.len, s.N, block0);
         if (it.poff >= 0) {
             const int64_t at = (int64_t)(it.poff + c) * s.n_kv + head;
 #pragma unroll
@@ -565,7 +567,7 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
 //
 // As above the scores are transposed, and which token is which row is chosen so that a lane's scores are the k-values that it
 // has to supply next: row 16 s + 8 b + 4 h + i of a half of the tile is its token 16 s + 8 h + 4 b + i, of granule 2 s + h.
-// The maximum is only raised when a score exceeds it by 2^kSlack: until then probabilities stay below 2^kSlack, which costs them nothing.
+// The maximum is only raised when a score exceeds it by kSlack: until then probabilities stay below 2^kSlack, 2^15 with the power that they are taken at.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
@@ -578,7 +580,7 @@ template <int DB>
 struct ManyLds {
     static constexpr int kUnits = kManyTile * DB * 4; // of 16 bytes, K's or V's of a tile
     u32x4 k[2][kUnits], v[2][kUnits];
-    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, u, 2^-u of each granule
+    float unit[2][kManyGranules], add[2][kManyGranules], less[2][kManyGranules]; // 2^ek, u + kManyUp, 2^-(u + kManyUp) of each granule
     PartPages pages;
 };
 
@@ -654,7 +656,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
             const int gk = min(g + (int)threadIdx.x, g1 - 1) - base, e = lds.pages.e[kv_div((uint32_t)gk, s.div_b)];
             const int ek = (int8_t)(e & 0xff), ev = e >> 8;
             lds.unit[buffer][threadIdx.x] = unit_of(ek);
-            const int u = units.of(ev);
+            const int u = units.of(ev) + kManyUp;
             lds.add[buffer][threadIdx.x] = (float)u;
             lds.less[buffer][threadIdx.x] = unit_of(-u);
         }
@@ -723,9 +725,9 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
             top = fmaxf(top, across_32(top));
-            const bool raise = top > kSlack || (m == -INFINITY && top > -INFINITY);
+            const bool raise = top > kSlack + kManyUp || (m == -INFINITY && top > -INFINITY);
             if (__any(raise)) {
-                const float by = raise ? top : 0.0f, m_new = raise ? so_far + by : m;
+                const float by = raise ? top - kManyUp : 0.0f, m_new = raise ? so_far + by : m;
                 const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-by); // (nothing has been added up before the first maximum)
                 m = m_new;
                 l *= keep;
@@ -766,7 +768,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     l += across_32(l);
     if (!real) return;
     // elements 32 k + 8 b + 4 h + i of column n are register 4 b + i of o[k]
-    const float by = l == 0.0f ? 0.0f : 1.0f / l, scale = units.scale(by, limit, s.N, block0); // a row that sees nothing is 0
+    const float by = l == 0.0f ? 0.0f : 1.0f / l, scale = units.scale(by, kManyUp, limit, s.N, block0); // a row that sees nothing is 0
 #pragma unroll
     for (int k = 0; k < DB; ++k)
 #pragma unroll

@@ -93,3 +93,29 @@ def test_v_of_blocks_far_apart(large, small, old, n, G):
         attend_with_weights(t, batch, [0], [n])
         if n == 1:
             t.attend(batch, 0, [0], [n], size=6.0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,bits,size", [(1, 24.25, 6000), (1, 28.25, 120), (40, 20.25, 6000), (40, 26.25, 6000)])
+def test_many_small_probabilities_beside_a_large_one(n, bits, size, dtype):
+    """A token of great score whose V is in one element, others of 2^-bits of its probability whose V is in another: slora.h promises 11 bits of a
+    probability down to 2^-21 of the largest, and multiples of 2^-31 of that below"""
+    D, large = 64, 1024.0
+    with Twin(512, D, 1, 1, dtype, max_seqs=1, max_tokens=size + n) as t:
+        rows = torch.zeros((size + n, 2, 1, D), dtype=t.dtype, device="cuda")
+        rows[0, 0, 0, 0] = 1.0
+        rows[0, 1, 0, 0] = large
+        rows[1:, 1, 0, 1] = large
+        t.step([0], [size], rows=rows[:size].contiguous())
+        batch = t.step([0], [n], rows=rows[size:].contiguous())
+        q = torch.zeros((n, D), dtype=t.dtype, device="cuda")
+        q[:, 0] = bits
+        out, _ = t.attend(batch, 0, [0], [n], q=q, scale=float(np.log(2.0)))
+        got = out[:, 1].double().cpu().numpy()
+        tokens = size + np.arange(n)  # of the small ones that each row sees
+        total = 1.0 + tokens * 2.0 ** -bits
+        ref = large * tokens * 2.0 ** -bits / total
+        # each rounded to 11 bits or to a multiple of 2^-31; q times log2 e and the exponential in fp32; one rounding of the output
+        each = max(2.0 ** -11 * 2.0 ** -bits, 2.0 ** -32) + 2.0 ** -bits * bits * 2.0 ** -20
+        bound = large * tokens * each / total + np.abs(ref) * (2.0 ** -11 if dtype == "f16" else 2.0 ** -8) + 2.0 ** -24
+        assert (np.abs(got - ref) <= bound).all(), (got[0], ref[0], bound[0])
