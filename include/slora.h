@@ -457,7 +457,8 @@ int32_t slora_kv8_append(slora_kv8_batch *batch, int32_t layer, const void *k, i
  * sequence; with causal != 0 those up to t's own slot.  q, out: DEVICE, row t at q + t * q_stride, [n_heads][head_dim] of
  * the pool's storage type, aligned as above; head h reads head h / (n_heads / n_kv_heads) of the cache.  A row that
  * sees no token is 0.  Products and sums are fp32; p times V's unit is rounded for the second product: to 11 bits
- * where it is at least 2^-21 of the row's largest, to multiples of 2^-31 of that below.  V of a block whose exponent is more than
+ * where it is at least 2^-21 of the row's largest, to multiples of 2^-31 of that below; to 22 bits and multiples of 2^-39 where a
+ * sequence's rows times the heads that share one of the cache are at most 32 (single and drafted tokens).  V of a block whose exponent is more than
  * 100 below the largest of the sequence may be read in units of 2^-100 of that one's (bfloat16 alone has such ranges).
  * weights_in, weights_out, pos: NULL, or DEVICE arrays [max_seqs][n_kv_heads][max_tokens] of this layer:
  *   weights_out[j] = weights_in[j] (0 for the batch's own tokens) + sum of p_j over the sequence's rows and the heads that share j's head,

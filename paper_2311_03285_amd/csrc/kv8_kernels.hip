@@ -211,8 +211,11 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
 //
 // Softmax: with scores s (times log2 e) and V's exponents ev, u = max(ev - top, -100) for the largest exponent `top` of the part, the
 // running maximum is of s + u, so that p = 2^(s + u - m) <= 1 is what the second product needs of V's units; the sum that
-// divides takes p * 2^-u.  p is the one number that is rounded, to binary16.  It is taken 2^15 times as large (2^7 times for prompts, whose maximum may be 2^8 behind), the
-// largest power that stays in range, so that 11 bits are kept down to 2^-29 (2^-21) of the largest.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
+// divides takes p * 2^-u.  p is the one number that is rounded, since that product takes 16-bit operands: for few columns to 22 bits, as two of binary16, which costs
+// half a percent where the cache's bytes are the bound (64 of 500 - 8000 tokens 123.9 us with one, 124.4 with two; 24 of 200 - 1500 60.0 / 60.4); for prompts to
+// the 11 bits of one, since two take a quarter longer (chunks of 128 - 1024 behind up to 4096 tokens 438 us / 539, a prompt of 512 29.5 / 31.6) and the output's own
+// rounding, to 11 or 8 bits, is as large.  p is taken 2^15 times as large (2^7 times for prompts, whose maximum may be 2^8 behind), the
+// largest power that stays in range, so that binary16 has its 11 bits down to 2^-29 (2^-21) of the largest.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
 // p >= 2^-100.  V of a block further below `top` is read in units of 2^(top - 100) instead of its own, which puts its elements off by less than 2^(top - 93).
 // A block with an infinity or NaN in V has u = 0, and the columns that see any of its tokens - their limits are behind its first one - get NaN at the end: the
 // scores' sum, which the weights are taken from, knows nothing of V.
@@ -477,12 +480,13 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         const float keep = __builtin_amdgcn_exp2f(m - m_use);
         m = m_new;
         float sum = 0.0f;
-        f16x8 p;
+        f16x8 p, rest;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float x = __builtin_amdgcn_exp2f(t[i] - (m_use - kFewUp));
             sum += x;
             p[i] = (_Float16)x;
+            rest[i] = (_Float16)(x - (float)p[i]);
         }
         l = __builtin_fmaf(l, keep, sum * unit_of(-u - kFewUp));
         if (__any(keep != 1.0f)) {
@@ -492,8 +496,11 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
         // element 32 k + 2 m + h of row m of o[2 k + h]
 #pragma unroll
         for (int k = 0; k < DB; ++k) {
-            o[2 * k] = mfma16(codes_to_f16x8(v[k].x, v[k].y), p, o[2 * k]);
-            o[2 * k + 1] = mfma16(codes_to_f16x8(v[k].z, v[k].w), p, o[2 * k + 1]);
+            const f16x8 v0 = codes_to_f16x8(v[k].x, v[k].y), v1 = codes_to_f16x8(v[k].z, v[k].w);
+            o[2 * k] = mfma16(v0, p, o[2 * k]);
+            o[2 * k + 1] = mfma16(v1, p, o[2 * k + 1]);
+            o[2 * k] = mfma16(v0, rest, o[2 * k]);
+            o[2 * k + 1] = mfma16(v1, rest, o[2 * k + 1]);
         }
     };
     int gr = g0 + wave * (kKvChunk / kKvGranule);

@@ -119,3 +119,33 @@ def test_many_small_probabilities_beside_a_large_one(n, bits, size, dtype):
         each = max(2.0 ** -11 * 2.0 ** -bits, 2.0 ** -32) + 2.0 ** -bits * bits * 2.0 ** -20
         bound = large * tokens * each / total + np.abs(ref) * (2.0 ** -11 if dtype == "f16" else 2.0 ** -8) + 2.0 ** -24
         assert (np.abs(got - ref) <= bound).all(), (got[0], ref[0], bound[0])
+
+
+@pytest.mark.parametrize("size,n,G", [(120, 1, 1), (5000, 1, 1), (700, 4, 8)])
+def test_probabilities_of_single_tokens_keep_22_bits(size, n, G):
+    """V of opposite signs for the two halves of the tokens, whose probabilities differ in bits that binary16 does not have: what is left of the sum is the difference"""
+    D = 64
+    with Twin(512, D, 1, G, "f16", max_seqs=1, max_tokens=size + n) as t:
+        rows = torch.zeros((size + n, 2, 1, D), dtype=t.dtype, device="cuda")
+        k = torch.from_numpy(t.rng.integers(-100, 101, (size + n) // 2)).to(t.dtype).cuda() / 64  # codes
+        rows[0:2 * len(k):2, 0, 0, 0] = k
+        rows[1:2 * len(k):2, 0, 0, 0] = k  # pairs of equal scores but for element 1
+        rows[1:2 * len(k):2, 0, 0, 1] = 1.0
+        rows[0::2, 1, 0, 0], rows[1::2, 1, 0, 0] = 1.0, -1.0
+        t.step([0], [size], rows=rows[:size].contiguous())
+        batch = t.step([0], [n], rows=rows[size:].contiguous())
+        q = torch.zeros((n, G * D), dtype=t.dtype, device="cuda")
+        q[:, 0::D] = 1.0
+        q[:, 1::D] = 2.0 ** -13  # the second of a pair has 1 + 2^-13 log 2 of the first's probability
+        out, _ = t.attend(batch, 0, [0], [n], q=q, scale=float(np.log(2.0)))
+        got = out.double().cpu().numpy().reshape(n, G, D)[:, :, 0]
+        score = rows[:, 0, 0, :2].double().cpu().numpy() @ [1.0, 2.0 ** -13]
+        sign = rows[:, 1, 0, 0].double().cpu().numpy()
+        for r in range(n):
+            seen = size + r + 1
+            p = np.exp2(score[:seen])
+            p /= p.sum()
+            ref = p @ sign[:seen]
+            # 2^-22 of each p; an fp32 argument of the exponential (scores below 2, log2 e in three factors) and its result, that sum's and the other's rounding: 2^-20 of each p is
+            # more than all; then one rounding of the output
+            assert (np.abs(got[r] - ref) <= 2.0 ** -20 + np.abs(ref) * 2.0 ** -11 + 2.0 ** -24).all(), (got[r], ref)
