@@ -369,6 +369,9 @@ __device__ __forceinline__ Units units_of(const PartPages &pp, int blocks)
     return {wave_max(top), spoiled};
 }
 
+// 1 / the scores' sum of a row.  One that sees no token is 0; one that does and has none in its sum has scores of -infinity alone, and no softmax.
+__device__ __forceinline__ float inverse_sum(float l, bool sees) { return l != 0.0f ? 1.0f / l : sees ? __uint_as_float(0x7fc00000u) : 0.0f; }
+
 // A part leaves its own average of V, whose units are its own, and {m, l}, its scores' sum as l * 2^m: l below 2^65 keeps l * 2^(m - the largest m) a
 // normal number wherever it matters (its u may have made it 2^100 times its share).
 __device__ __forceinline__ void put_sum(float *to, float m, float l)
@@ -541,8 +544,8 @@ __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void 
             for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(merge_o[k][c][d + i], x, sum[i]);
         }
         const int r = (it.a + c) / s.G;
-        const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
-        const float scale = units.scale(by, kFewUp, a.causal ? min(old + r + 1, q.len) : q.len, s.N, block0);
+        const int sees = a.causal ? min(old + r + 1, q.len) : q.len;
+        const float by = inverse_sum(total, it.poff < 0 && sees > 0), scale = units.scale(by, kFewUp, sees, s.N, block0);
         if (it.poff >= 0) {
             const int64_t at = (int64_t)(it.poff + c) * s.n_kv + head;
 #pragma unroll
@@ -775,7 +778,7 @@ __global__ __launch_bounds__(kKvManyThreads, DB <= 4 ? 2 : 1) void kv_attend_man
     l += across_32(l);
     if (!real) return;
     // elements 32 k + 8 b + 4 h + i of column n are register 4 b + i of o[k]
-    const float by = l == 0.0f ? 0.0f : 1.0f / l, scale = units.scale(by, kManyUp, limit, s.N, block0); // a row that sees nothing is 0
+    const float by = inverse_sum(l, it.poff < 0 && limit > 0), scale = units.scale(by, kManyUp, limit, s.N, block0);
 #pragma unroll
     for (int k = 0; k < DB; ++k)
 #pragma unroll
@@ -857,8 +860,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvItem *__restrict__
             for (int i = 0; i < kPer; ++i) sum[i] += merge[w][lane + 64 * i];
         }
     }
-    const float by = total == 0.0f ? 0.0f : 1.0f / total; // a row that sees nothing is 0
-    const int r = (it.a + c) / s.G, h = head * s.G + (it.a + c) % s.G;
+    const int r = (it.a + c) / s.G;
+    const float by = inverse_sum(total, (a.causal ? min(q.len - q.rows + r + 1, q.len) : q.len) > 0);
+    const int h = head * s.G + (it.a + c) % s.G;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
         if (lane + 64 * i < D) a.out[(int64_t)(q.row0 + r) * a.out_stride + (int64_t)h * D + lane + 64 * i] = narrow<DT>(sum[i] * by);

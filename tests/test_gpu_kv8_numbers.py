@@ -149,3 +149,20 @@ def test_probabilities_of_single_tokens_keep_22_bits(size, n, G):
             # 2^-22 of each p; an fp32 argument of the exponential (scores below 2, log2 e in three factors) and its result, that sum's and the other's rounding: 2^-20 of each p is
             # more than all; then one rounding of the output
             assert (np.abs(got[r] - ref) <= 2.0 ** -20 + np.abs(ref) * 2.0 ** -11 + 2.0 ** -24).all(), (got[r], ref)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("old,n,G", [(20, 1, 2), (1500, 1, 2), (20, 40, 2), (1500, 40, 2)])
+def test_an_infinite_query_gives_nan_and_not_zero(old, n, G, sign, dtype):
+    """all scores of a row that sees tokens are the same infinity: there is no softmax, and 0 is for rows that see none"""
+    with Twin(512, 32, 1, G, dtype, max_seqs=1, max_tokens=1600) as t:
+        rows = t.rows(old + n)
+        rows[:, 0, :, 5] = 1.0
+        t.step([0], [old], rows=rows[:old].contiguous())
+        batch = t.step([0], [n], rows=rows[old:].contiguous())
+        q = torch.from_numpy(t.rng.standard_normal((n, G * 32))).to(t.dtype).cuda()
+        q[n // 2, 32 + 5] = sign * float("inf")
+        out, _ = attend_with_weights(t, batch, [0], [n], q=q)
+        nan = torch.isnan(out)
+        assert nan[n // 2, 32:].all() and int(nan.sum()) == 32
