@@ -245,6 +245,14 @@ __device__ __forceinline__ int element_of(int j, int g)
     return j / 2 * 2 + 1 < DB ? j / 2 * 64 + 16 * g + 8 * (j % 2) : j * 32 + 8 * g;
 }
 
+// q of bfloat16 in the range of binary16: its largest magnitude has exponent bits x, and times 2^(141 - x) lies in [2^14, 2^15).  The power is kept
+// where its inverse is a normal number too; an infinity or NaN stays what it is.
+__device__ __forceinline__ int power_for_f16(uint32_t top)
+{
+    const int x = (int)(top >> 7);
+    return x == 255 ? 0 : min(141 - x, 126);
+}
+
 // q of one column as second operands, element(j) on for step j, and the power of two to multiply its scores by.  Lanes that differ in the bits
 // of LANES hold other elements of the same column.
 template <int DT, int STEPS, int LANES, typename F>
@@ -266,9 +274,7 @@ __device__ __forceinline__ void load_column(const uint16_t *q, F element, f16x8 
 #pragma unroll
         for (int x = 16; x < kWave; x *= 2)
             if (LANES & x) top = max(top, (uint32_t)__shfl_xor((int)top, x, kWave));
-        // largest magnitude 2^(x - 127) .. : times 2^(141 - x) it lies in [2^14, 2^15); both powers are kept normal numbers
-        const int x = (int)(top >> 7);
-        const int up = x == 0 || x == 255 ? 0 : min(max(141 - x, -100), 100);
+        const int up = power_for_f16(top);
         const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
         unit = __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
@@ -963,7 +969,7 @@ __global__ __launch_bounds__(256) void kv_weights_kernel(const KvSeq *__restrict
             for (int k = 0; k < DB; ++k) top = max(max(top, max(raw[k].x & 0x7fffu, (raw[k].x >> 16) & 0x7fffu)), max(raw[k].y & 0x7fffu, (raw[k].y >> 16) & 0x7fffu));
 #pragma unroll
             for (int x = 1; x < 8; x *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, x, kWave));
-            const int x = (int)(top >> 7), up = x == 0 || x == 255 ? 0 : min(max(141 - x, -100), 100);
+            const int up = power_for_f16(top);
             scale = __uint_as_float((uint32_t)(127 + up) << 23);
             unit = __uint_as_float((uint32_t)(127 - up) << 23);
         }

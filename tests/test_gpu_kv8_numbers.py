@@ -166,3 +166,13 @@ def test_an_infinite_query_gives_nan_and_not_zero(old, n, G, sign, dtype):
         out, _ = attend_with_weights(t, batch, [0], [n], q=q)
         nan = torch.isnan(out)
         assert nan[n // 2, 32:].all() and int(nan.sum()) == 32
+
+
+@pytest.mark.parametrize("n", [1, 12, 40])
+@pytest.mark.parametrize("power", [-120, -110, 114, 118])
+def test_queries_at_the_ends_of_bfloat16(power, n):
+    """what the scale makes ordinary scores of"""
+    with Twin(512, 64, 1, 2, "bf16", max_seqs=2, max_tokens=120) as t:
+        t.step([0, 1], [60, 9])
+        batch = t.step([0, 1], [n, n])
+        attend_with_weights(t, batch, [0, 1], [n, n], size=2.0 ** power, scale=2.0 ** (-3 - power))
