@@ -106,7 +106,7 @@ int32_t slora_pool_stats(const slora_pool *pool, int64_t *out, int32_t n);
  * Sec. 5.1, Fig. 3: KV-cache vectors and adapter weights are interleaved in one pool of
  * H-vector pages.
  * KV pages can never be given to an adapter; the LoRA kernels never read or write them.
- * Errors: ERANGE (index), EBUSY (page owned by an adapter, or listed twice).
+ * Errors: ERANGE (index), EBUSY (page owned by an adapter, or by an 8-bit KV cache (slora_kv8_extend), or listed twice).
  */
 int32_t slora_pool_mark_kv(slora_pool *pool, const int32_t *page_idx, int64_t n, int32_t owned);
 

@@ -32,6 +32,12 @@ int32_t check_seqs(const slora_kv8 *cache, int32_t n, const int32_t *seqs)
     return SLORA_OK;
 }
 
+void release(slora_pool *pool, int32_t page)
+{
+    pool->in_cache[(size_t)page] = 0;
+    pool->set_state(page, kFree);
+}
+
 // Workgroups that a launch of attention is cut into, if the sequences are long enough: twice three for every compute unit.  us a pass with 768, 1536, 2048,
 // 4096: 24 sequences of 200 - 1500 tokens 64.2 / 59.6 / 59.2 / 63.3, 64 of 500 - 8000 129 / 126 / 125 / 137, two of 90000 - 131000 86.8 / 84.9 / 91.0 / 108.
 constexpr int64_t kPartTarget = 1536;
@@ -249,6 +255,7 @@ int32_t slora_kv8_init(slora_kv8 **out, slora_pool *pool, int32_t n_layers, int3
     if (rc == SLORA_OK) {
         try {
             c->seqs.resize((size_t)max_seqs);
+            pool->in_cache.resize((size_t)pool->n_pages);
         } catch (const std::bad_alloc &) {
             rc = fail(SLORA_ENOMEM, "out of host memory");
         }
@@ -284,7 +291,7 @@ int32_t slora_kv8_destroy(slora_kv8 *c)
         (void)hipFree(c->d_table);
     }
     for (auto &q : c->seqs)
-        for (int32_t p : q.pages) c->pool->set_state(p, kFree);
+        for (int32_t p : q.pages) release(c->pool, p);
     c->pool->live_caches--;
     delete c;
     return SLORA_OK;
@@ -360,6 +367,7 @@ int32_t slora_kv8_extend(slora_kv8 *c, int32_t n, const int32_t *seqs, const int
         rc = pool->take(want, kKv, pages.data());
         if (rc != SLORA_OK) return rc;
     }
+    for (int32_t p : pages) pool->in_cache[(size_t)p] = 1;
     const int32_t *at = pages.data();
     for (int32_t i = 0; i < n; ++i) {
         auto &q = c->seqs[(size_t)seqs[i]];
@@ -387,7 +395,7 @@ int32_t slora_kv8_truncate(slora_kv8 *c, int32_t n, const int32_t *seqs, const i
         auto &q = c->seqs[(size_t)seqs[i]];
         if (lengths[i] == q.len) continue;
         const size_t stay = (size_t)c->blocks(lengths[i]) * c->per_block();
-        for (size_t k = stay; k < q.pages.size(); ++k) c->pool->set_state(q.pages[k], kFree);
+        for (size_t k = stay; k < q.pages.size(); ++k) release(c->pool, q.pages[k]);
         c->pages_held -= (int64_t)(q.pages.size() - stay);
         q.pages.resize(stay);
         if (!evicted) q.seen -= q.len - lengths[i];

@@ -479,6 +479,10 @@ int32_t slora_pool_mark_kv(slora_pool *pool, const int32_t *page_idx, int64_t n,
             rc = fail(SLORA_EBUSY, "page %lld is owned by an adapter", (long long)p);
             break;
         }
+        if (!pool->in_cache.empty() && pool->in_cache[(size_t)p]) {
+            rc = fail(SLORA_EBUSY, "page %lld is owned by an 8-bit KV cache", (long long)p);
+            break;
+        }
         pool->state[p] = s | kSeen;
     }
     const int64_t marked = i;

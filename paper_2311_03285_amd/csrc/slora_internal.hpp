@@ -201,6 +201,7 @@ struct slora_pool {
     uint64_t unload_generation = 0;
     int64_t live_plans = 0;
     int64_t live_caches = 0;                          // 8-bit KV caches on its pages
+    std::vector<uint8_t> in_cache;                    // of each KV page, whether it is one of theirs (empty before the first cache)
     int64_t mfma_min_tokens = 16;
     int64_t mfma_min_tiles = 32;
     int64_t xcd_group = 0;                            // accepted, no effect
