@@ -390,7 +390,7 @@ typedef struct slora_kv8_batch slora_kv8_batch; /* one batch's work lists and sc
  * of `pool`.  n_heads query heads share n_kv_heads heads of K and V (n_heads % n_kv_heads == 0);
  * head_dim is 32, 64, 96, 128, 192 or 256 and at most page_H / 8.  dev_exps: DEVICE memory of the caller
  * (borrowed like the pool's), max_seqs * ceil(max_tokens / N) * n_layers * n_kv_heads * 2 bytes: the
- * signed exponents [sequence][block][layer][head][K, V]; no particular content.  NULL for a host-only
+ * signed exponents [sequence][block][layer][head][K, V]; 2-byte aligned, no particular content.  NULL for a host-only
  * pool.  The library allocates the page table, 4 bytes for every two of those.
  * slora_kv8_destroy waits for the device and releases the pages of all sequences; its batches must
  * have been destroyed (EBUSY), and a pool is destroyed after its caches (EBUSY).

@@ -236,6 +236,7 @@ int32_t slora_kv8_init(slora_kv8 **out, slora_pool *pool, int32_t n_layers, int3
     if (max_seqs < 1 || max_seqs > 65535) return fail(SLORA_EINVAL, "max_seqs=%d must be in [1, 65535]", max_seqs);
     if (max_tokens < 1 || max_tokens > 1 << 27) return fail(SLORA_EINVAL, "max_tokens=%d must be in [1, 2^27]", max_tokens);
     if (pool->dev_base && !dev_exps) return fail(SLORA_EINVAL, "dev_exps is NULL");
+    if (reinterpret_cast<uintptr_t>(dev_exps) & 1) return fail(SLORA_EINVAL, "dev_exps must be 2-byte aligned"); // (K's and V's are read together)
     slora_kv8 *c = new (std::nothrow) slora_kv8;
     if (!c) return fail(SLORA_ENOMEM, "out of host memory");
     c->pool = pool;

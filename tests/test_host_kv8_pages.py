@@ -40,3 +40,9 @@ def test_pages_of_a_cache_are_nobody_elses(cache):
     slora.pool_mark_kv(pool, np.arange(100, 120))
     slora.pool_mark_kv(pool, np.arange(100, 120), False)
     assert slora.pool_free_pages(pool) == 200 - 2 - 2
+
+
+def test_exponents_that_are_not_aligned(cache):
+    pool, _ = cache
+    refused(slora.EINVAL, slora.kv8_init, pool, 1, 2, 2, 64, 4, 100, 4097)
+    slora.kv8_destroy(slora.kv8_init(pool, 1, 2, 2, 64, 4, 100, 4098))
