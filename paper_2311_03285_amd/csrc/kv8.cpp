@@ -338,7 +338,8 @@ int32_t slora_kv8_extend(slora_kv8 *c, int32_t n, const int32_t *seqs, const int
         pages.resize((size_t)want);
         for (int32_t i = 0; i < n; ++i) {
             auto &q = c->seqs[(size_t)seqs[i]];
-            q.pages.reserve((size_t)c->blocks(q.len + tokens[i]) * c->per_block());
+            const size_t need = (size_t)c->blocks(q.len + tokens[i]) * c->per_block();
+            if (need > q.pages.capacity()) q.pages.reserve(std::max(need, 2 * q.pages.capacity())); // (it grows by a block at a time)
         }
     } catch (const std::bad_alloc &) {
         return fail(SLORA_ENOMEM, "out of host memory");
