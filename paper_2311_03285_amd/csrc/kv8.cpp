@@ -539,7 +539,8 @@ int32_t slora_kv8_attend(slora_kv8_batch *b, int32_t layer, const void *q, int64
     if (weights && (!weights_in || !weights_out || !pos)) return fail(SLORA_EINVAL, "weights_in, weights_out and pos go together");
     if (weights && ((reinterpret_cast<uintptr_t>(weights_in) | reinterpret_cast<uintptr_t>(weights_out) | reinterpret_cast<uintptr_t>(pos)) & 3))
         return fail(SLORA_EINVAL, "weights_in, weights_out and pos must be 4-byte aligned");
-    if (!std::isfinite(scale)) return fail(SLORA_EINVAL, "scale must be finite");
+    const float by = scale * 1.44269504088896340736f; // (scores are powers of two)
+    if (!std::isfinite(by)) return fail(SLORA_EINVAL, "scale must be finite, and its product with log2 e");
     const slora_kv8 *c = b->cache;
     const int64_t width = (int64_t)c->n_heads * c->D;
     if (b->rows > 0 && ((rc = check_rows("q", q, q_stride, width)) != SLORA_OK || (rc = check_rows("out", out, out_stride, width)) != SLORA_OK)) return rc;
@@ -558,7 +559,7 @@ int32_t slora_kv8_attend(slora_kv8_batch *b, int32_t layer, const void *q, int64
     a.out = static_cast<uint16_t *>(out);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    a.scale = scale * 1.44269504088896340736f;
+    a.scale = by;
     a.causal = causal != 0;
     a.scores = weights ? b->set->v : nullptr;
     a.part_o = b->set->v + score_floats;
