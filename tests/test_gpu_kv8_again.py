@@ -1,0 +1,57 @@
+"""Attention over the 8-bit cache called again: the same bits, whatever the form; weights added up in place as well as beside."""
+import numpy as np
+import pytest
+import torch
+
+from kv8_util import Twin
+from paper_2311_03285_amd import slora
+
+pytestmark = pytest.mark.gpu
+
+# old tokens, new tokens, heads that share one of the cache: one part or several, few columns and many, weights from kept scores and from K again
+FORMS = [(100, 1, 2), (3000, 1, 2), (3000, 4, 4), (300, 12, 2), (200, 40, 2), (5000, 70, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("old,n,G", FORMS)
+def test_weights_in_place(old, n, G, dtype):
+    with Twin(1024, 64, 2, G, dtype, max_seqs=2, max_tokens=old + n + 90) as t:
+        t.step([1, 0], [old, 77])
+        batch = t.step([1, 0], [n, 1])
+        w, _, pos = t.weight_arrays()
+        before = w.cpu().numpy().copy()
+        t.attend(batch, 0, [1, 0], [n, 1], weights=(w, w, pos))
+        after = w.cpu().numpy()
+        for s, m in ((1, n), (0, 1)):
+            size = t.len[s]
+            for h in range(t.kv):
+                total, slack = t.drawn[s, h]
+                ref = total.copy()
+                ref[:size - m] += before[s, h, :size - m]
+                assert (np.abs(after[s, h, :size] - ref) <= slack + np.abs(ref) * 2.0 ** -22).all(), (s, h)
+                assert np.array_equal(after[s, h, size:], before[s, h, size:])
+                assert np.array_equal(pos[s, h, size - m:size].cpu().numpy(), np.arange(size - m, size))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("old,n,G", FORMS)
+def test_a_call_repeated_gives_the_same_bits(old, n, G, dtype):
+    with Twin(1024, 64, 2, G, dtype, max_seqs=2, max_tokens=old + n + 90) as t:
+        t.step([1, 0], [old, 77])
+        batch = t.step([1, 0], [n, 1])
+        w, w_out, pos = t.weight_arrays()
+        width = t.kv * t.G * t.D
+        q = torch.from_numpy(t.rng.standard_normal((n + 1, width))).to(t.dtype).cuda()
+        out = torch.empty_like(q)
+        first = None
+        for _ in range(4):
+            out.fill_(9.0)
+            w_out.fill_(-1.0)
+            slora.kv8_attend(batch, 0, q.data_ptr(), width, out.data_ptr(), width, 0.125, True, [x.data_ptr() for x in (w, w_out, pos)])
+            torch.cuda.synchronize()
+            if first is None:
+                first = out.clone(), w_out.clone()
+            assert torch.equal(out, first[0]) and torch.equal(w_out, first[1])
+            slora.kv8_attend(batch, 0, q.data_ptr(), width, out.data_ptr(), width, 0.125, True)  # without weights: the same outputs
+            torch.cuda.synchronize()
+            assert torch.equal(out, first[0])
