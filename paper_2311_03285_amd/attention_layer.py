@@ -63,14 +63,36 @@ class AttentionLayer:
             slora.adapter_upload(self.pool, a, self.adapters[a].data_ptr())
 
     def step(self, seqs: Sequence[int], tokens: Sequence[int], adapters: Sequence[int], x: torch.Tensor) -> List[torch.Tensor]:
-        """x: [sum of tokens, H], new tokens of `seqs` (whose adapters are given); returns every layer's output, each layer reading the one before."""
-        H, D = self.H, self.D
+        """x: [sum of tokens, H], new tokens of `seqs` (whose adapters are given); returns every layer's output, each layer reading the one before.
+        A step that is refused (an adapter that is not loaded, no pages left) leaves the sequences as they were."""
+        if x.shape != (sum(tokens), self.H) or x.dtype != self.dtype or x.device != self.pages.device or not x.is_contiguous():
+            raise ValueError(f"x must be [{sum(tokens)}, {self.H}] of {self.dtype} on {self.pages.device}, row after row")
+        if not len(seqs) == len(tokens) == len(adapters):
+            raise ValueError("as many tokens and adapters as sequences")
+        before = slora.kv8_lengths(self.cache, seqs)
         slora.kv8_extend(self.cache, seqs, tokens)
-        keep = np.minimum(slora.kv8_lengths(self.cache, seqs), self.budget)
-        batch = slora.kv8_batch_plan(self.cache, seqs, tokens, keep)
-        plan = slora.batch_plan(self.pool, np.repeat(np.asarray(adapters, np.int32), tokens), np.concatenate([[0], np.cumsum(tokens)]))
-        T, stream = x.shape[0], torch.cuda.current_stream()
-        evicts = bool((keep < slora.kv8_lengths(self.cache, seqs)).any())
+        batch = plan = None
+        try:
+            lengths = slora.kv8_lengths(self.cache, seqs)
+            keep = np.minimum(lengths, self.budget)
+            evicts = bool((keep < lengths).any())
+            batch = slora.kv8_batch_plan(self.cache, seqs, tokens, keep)
+            plan = slora.batch_plan(self.pool, np.repeat(np.asarray(adapters, np.int32), tokens), np.concatenate([[0], np.cumsum(tokens)]))
+            outputs = self._layers(batch, plan, x, evicts)
+        except Exception:
+            slora.kv8_truncate(self.cache, seqs, before)  # (what is refused is refused before anything is launched)
+            raise
+        finally:
+            if plan is not None:
+                slora.plan_destroy(plan)
+            if batch is not None:
+                slora.kv8_batch_destroy(batch)
+        if evicts:
+            slora.kv8_truncate(self.cache, seqs, keep, evicted=True)
+        return outputs
+
+    def _layers(self, batch, plan, x: torch.Tensor, evicts: bool) -> List[torch.Tensor]:
+        H, D, T, stream = self.H, self.D, x.shape[0], torch.cuda.current_stream()
         outputs = []
         for layer in range(self.layers):
             q, k, v, a, out = (torch.empty((T, H), dtype=self.dtype, device=x.device) for _ in range(5))
@@ -87,10 +109,6 @@ class AttentionLayer:
                 slora.kv8_evict(batch, layer, self.recent, w, w, p, p, stream)
             outputs.append(out)
             x = out
-        slora.plan_destroy(plan)
-        slora.kv8_batch_destroy(batch)
-        if evicts:
-            slora.kv8_truncate(self.cache, seqs, keep, evicted=True)
         return outputs
 
     def finish(self, seqs: Sequence[int]) -> None:
