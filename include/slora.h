@@ -423,7 +423,8 @@ int32_t slora_kv8_extend(slora_kv8 *cache, int32_t n, const int32_t *seqs, const
  * Cut sequence seqs[i] to lengths[i] tokens, at most what it holds, and free the pages of whole blocks
  * behind them.  evicted == 0: the last tokens are dropped, as after drafted tokens that were refused
  * (their positions are given out again).  evicted != 0: slora_kv8_evict has moved the tokens that stay to
- * the front in every layer; positions go on from where they were.  Batches planned before with such a
+ * the front in every layer; positions go on from where they were.  A sequence that is left with no tokens is a new one, whose
+ * positions begin at 0.  Batches planned before with such a
  * sequence become stale (EBUSY).  Launches in flight keep reading the freed pages: the caller orders
  * their completion before other streams write them.
  */

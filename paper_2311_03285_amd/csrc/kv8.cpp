@@ -38,14 +38,22 @@ void release(slora_pool *pool, int32_t page)
     pool->set_state(page, kFree);
 }
 
-// Workgroups that a launch of attention is cut into, if the sequences are long enough: twice three for every compute unit.  us a pass with 768, 1536, 2048,
-// 4096: 24 sequences of 200 - 1500 tokens 64.2 / 59.6 / 59.2 / 63.3, 64 of 500 - 8000 129 / 126 / 125 / 137, two of 90000 - 131000 86.8 / 84.9 / 91.0 / 108.
+// Workgroups that a launch of attention is cut into, if the sequences are long enough: twice three for every compute unit.  No one number is best for all.  us of append
+// and attention, from two runs, with 768, 1024, 1536, 2048, 4096 (cached heads / heads that share one):
+//   24 sequences of 200 - 1500 tokens (40 / 1)  65.3  61.2  60.4  59.2  63.3      six of 15000 - 25000 (8 / 8)   58.4  57.0  58.0  60.0  69.7
+//   64 of 500 - 8000 (8 / 8)                     128   126   125   125   137       12 of 5000 (8 / 4)             31.4  34.1  34.3  33.3  42.2
+//   two of 90000 - 131000 (8 / 8)                 88    88    86    91   108       one of 30000 (8 / 8)           25.1  27.2  33.5  38.2  38.2
+//   100 of 300 - 1600 (8 / 4)                   47.0  46.6  46.7  48.2  55.1      three of 9000 (32 / 1)         45.5  49.0  47.1  47.7  50.0
+// Fewer and longer parts spare the join where few sequences are cut, more even out sequences of different lengths.
 constexpr int64_t kPartTarget = 1536;
 // Prompts, two workgroups of which fit a compute unit: us a pass with 256, 512, 1024 workgroups: a chunk of 512 behind 30000 983 / 741 / 743, eight of 64 behind
 // 4000 147 / 134 / 151, one of 2048 98 / 98 / 118; parts of at least 128, 256, 512 tokens, a prompt of 512: 37.5 / 35.7 / 33.8.
 constexpr int64_t kManyTarget = 512;
 constexpr int32_t kManyLeast = 64;
-constexpr int32_t kPartLeast = 16; // granules: a chunk for each of the four wavefronts
+// Granules, a chunk for each of the four wavefronts.  us with parts of at least 8, 16, 32, 64: one sequence of 400 tokens (32 / 1) 12.2 / 12.0 / 12.7 / 11.7, of 1500 13.8 / 14.6 / 14.1
+// / 15.5, of 2000 (8 / 4) 12.9 / 14.2 / 14.0 / 15.3; four of 1000 (8 / 4) 15.0 / 13.4 / 13.7 / 15.3; 40 of 100 - 400 (8 / 1) 16.1 / 13.5 / 13.6 / 12.2; eight of four drafted tokens
+// behind 600 (4 / 4) 13.8 / 12.3 / 12.5 / 12.9.  Batches that fill the card uncut lose by being cut: 32 of 700 (8 / 8) 24.0 / 24.1 / 20.0 / 19.1, 128 of 64 - 500 (8 / 4) 29.5 / 29.6 / 27.5 / 24.8.
+constexpr int32_t kPartLeast = 16;
 
 } // namespace
 

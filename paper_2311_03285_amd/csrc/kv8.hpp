@@ -37,7 +37,6 @@ struct KvSeq {
 };
 static_assert(sizeof(KvSeq) == 48, "KvSeq must stay 48 bytes");
 
-// work of one workgroup per head
 // work of one workgroup, for each head of the cache
 struct KvItem {
     int32_t s;    // sequence of the batch

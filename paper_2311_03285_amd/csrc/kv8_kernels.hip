@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attention_device.hpp"
 #include "kv8.hpp"
 
 namespace slora {
@@ -19,25 +20,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kWave = 64;
-
-template <int DT>
-__device__ __forceinline__ float widen(uint16_t b)
-{
-    return DT == SLORA_F16 ? (float)__builtin_bit_cast(_Float16, b) : __uint_as_float((uint32_t)b << 16);
-}
-template <int DT>
-__device__ __forceinline__ uint16_t narrow(float f)
-{
-    if constexpr (DT == SLORA_F16)
-        return __builtin_bit_cast(uint16_t, (_Float16)f);
-    else
-        return __builtin_bit_cast(uint16_t, (__bf16)f);
-}
-
-// the wavefront's number in its workgroup, as a scalar: what follows from it takes no vector instructions
-__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave); }
 
 __device__ __forceinline__ float across_16(float v) { return __shfl_xor(v, 16, kWave); }
 __device__ __forceinline__ float across_32(float v) { return __shfl_xor(v, 32, kWave); }
@@ -390,8 +372,8 @@ __device__ __forceinline__ void put_sum(float *to, float m, float l)
 // A workgroup = one item: up to 16 columns x a part of the sequence; the wavefronts take chunks of 32 tokens in turn, keep their own
 // maxima, sums and O', and are put together in LDS at the end.
 // Bound: HBM, from which the cache comes once, with non-temporal loads (645 MB of 64 sequences, 8 heads: 115 us = 5.6 TB/s, with plain loads 125; 227 MB of
-// 24 sequences, 40 heads: 46 us = 4.9 TB/s); a single sequence of 701 tokens takes 5.3 us, the chain of page, K, score, sum.  Vector units 40 %, matrix
-// units 6 % busy even where one column of sixteen is in use, so there is no kernel of its own for one.
+// 24 sequences, 40 heads: 46 us = 4.9 TB/s); a single sequence of 701 tokens takes 5.6 us, the chain of page, K, score, sum.  Vector units 43 - 45 %, matrix
+// units 9 - 10 % busy even where one column of sixteen is in use, so there is no kernel of its own for one.
 template <int DT, int DB>
 __global__ __launch_bounds__(kKvFewThreads, DB <= 4 ? 3 : DB == 6 ? 2 : 1) void kv_attend_few_kernel(const KvItem *__restrict__ items, const KvSeq *__restrict__ seqs, KvShape s, KvAttend a)
 {
@@ -590,7 +572,7 @@ __device__ __forceinline__ f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f
 constexpr int kManyTile = kKvManyTile, kManyGranules = kManyTile / kKvGranule;
 constexpr float kSlack = 8.0f;
 
-// Bound: the vector units, 12 of whose instructions go beside each matrix instruction (over half of all cycles, at four an instruction; matrix units 35 %): a chunk of 512 behind 30000 tokens, 64 heads 627 us = 810 TFLOP/s, chunks of 128 - 1024 behind up to 4096 426 us.
+// Bound: the vector units, 12 of whose instructions go beside each matrix instruction (over half of all cycles, at four an instruction; matrix units 35 %): a chunk of 512 behind 30000 tokens, 64 heads 680 us = 750 TFLOP/s, chunks of 128 - 1024 behind up to 4096 426 - 440 us.
 // Two workgroups share a compute unit up to 128 elements a head, so that one's products run beside the other's softmax.
 template <int DB>
 struct ManyLds {
@@ -911,7 +893,7 @@ __global__ __launch_bounds__(256) void kv_weights_few_kernel(const KvSeq *__rest
 // 8 b + 4 h + i of the 32 x 32 instruction is its token of that number, of granule b); the workgroup's four go through the columns together,
 // 32 at a time, which are put into LDS as binary16 while the ones before are worked on.  A lane adds up its tokens over its column of
 // every tile; the 32 columns are added at the end.
-// Bound: vector units (an exponential and two products for each score); a chunk of 512 behind 30000 tokens, 64 heads 510 us beside attention's 627.
+// Bound: vector units (an exponential and two products for each score); a chunk of 512 behind 30000 tokens, 64 heads 605 us beside attention's 680.
 template <int DB>
 struct WeightsLds {
     u32x4 q[2][DB * 4 * 32]; // [8 elements][column]
@@ -1524,12 +1506,6 @@ __global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const KvSeq
             }
         }
     }
-}
-
-int32_t check_launch(const char *what)
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? SLORA_OK : fail(SLORA_EHIP, "launching %s: %s", what, hipGetErrorString(e));
 }
 
 // f(integral constants of the type and of D / 32)

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attention_device.hpp"
 #include "w4.hpp"
 
 namespace slora {
@@ -17,22 +18,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kWave = 64;
-
-template <int DT>
-__device__ __forceinline__ float widen(uint16_t b)
-{
-    return DT == SLORA_F16 ? (float)__builtin_bit_cast(_Float16, b) : __uint_as_float((uint32_t)b << 16);
-}
-template <int DT>
-__device__ __forceinline__ uint16_t narrow(float f)
-{
-    if constexpr (DT == SLORA_F16)
-        return __builtin_bit_cast(uint16_t, (_Float16)f);
-    else
-        return __builtin_bit_cast(uint16_t, (__bf16)f);
-}
 
 // ---------------------------------------------------------------------------------------
 // packing
@@ -110,9 +95,6 @@ struct Operand<SLORA_BF16> {
 };
 
 __device__ __forceinline__ int token_of_row(int m) { return 4 * (m % 4) + m / 4; }
-
-// the wavefront's number in its workgroup, as a scalar
-__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave); }
 
 // Up to four tokens.  A workgroup = RT tiles of 16 outputs; its WV wavefronts take chunks of 128 inputs in turn, with the weights of the next ones and x of the
 // next one under way, and are added in LDS.  Loads are not behind branches where others are waited for: the compiler would wait for all of them.
@@ -230,7 +212,7 @@ __global__ __launch_bounds__(WV *kWave) void w4_kernel(W4Args a, bool y16)
 // bytes, its pieces of 16 bytes permuted by its number, so that the 16 rows of an operand are in different banks).  While a chunk is
 // worked on, the team's next one goes from registers to the other buffer, the one after that from memory to
 // registers; the barrier between chunks waits for LDS alone.
-// Two of 20480 of 5120, 32 tokens 37 us = 360 TFLOP/s and 3.2 TB/s; three of 5003 of 3080, 67 tokens, groups of 32 25 us.  Bound: no unit alone - of the former's
+// Two of 20480 of 5120, 32 tokens 37 - 39 us = 340 - 360 TFLOP/s and 3.0 - 3.2 TB/s; three of 5003 of 3080, 67 tokens, groups of 32 25 - 26 us.  Bound: no unit alone - of the former's
 // cycles the vector units are busy for 35 % (at four an instruction), the matrix units, half of whose work takes the zeros off, for 26 %.
 constexpr int kWideThreads = 8 * kWave;
 
@@ -247,7 +229,7 @@ __global__ __launch_bounds__(kWideThreads, TEAMS == 2 && RT == 1 && NT <= 2 && (
     typedef typename Operand<DT>::type operand;
     constexpr int kPer = kW4Chunk / U, kRows = NT * 16, kPieces = kW4Chunk / 8;
     // Chunks of weights under way.  Two, and with them registers for three workgroups of a compute unit, are as fast as four and two workgroups, or faster: two of
-    // 20480 of 5120, 32 tokens 44.4 -> 39.2 us, where two at a time go through 640 workgroups in one round and a quarter.
+    // 20480 of 5120, 32 tokens 39.2 us with two, 44.4 with four, where two at a time go through 640 workgroups in one round and a quarter.
     constexpr int kAhead = 2;
     constexpr int kMembers = 8 / TEAMS;     // wavefronts of a team,
     constexpr int kPuts = NT * 4 / kMembers; // each of which puts four rows at a time into LDS, so often
@@ -398,12 +380,6 @@ __global__ __launch_bounds__(kWideThreads, TEAMS == 2 && RT == 1 && NT <= 2 && (
         }
 }
 
-int32_t check_launch(const char *what)
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? SLORA_OK : fail(SLORA_EHIP, "launching %s: %s", what, hipGetErrorString(e));
-}
-
 // workgroups of `each` tiles of outputs
 int64_t share_out(W4Args &a, int each)
 {
@@ -435,8 +411,10 @@ int32_t launch_wide(W4Args &a, bool y16, void *stream)
 // Teams: the fewer workgroups of 16 outputs there are, the more of its eight wavefronts share out a workgroup's inputs.  us with 2, 4, 8 teams: 1024
 // outputs of 8192 inputs, two matrices, 32 tokens 23.2 / 15.2 / 13.0; 4096 of 4096, 32 tokens 12.7 / 10.3 / 10.0; 8192 of 8192, 32 tokens
 // 22.7 / 16.3 / 24.5; four of 4096 of 4096, 16 tokens 12.0 / 12.5 / 17.8.  (Eight teams' x of more than 32 tokens does not fit LDS.)
-// Two tiles of outputs a wavefront where x is read for 33 - 48 tokens: three of 5003 of 3080, 67 tokens 33.3 -> 28.1; with 64, four of 8192 of
-// 8192 69.6 / 71.8, and with 32, two of 20480 of 5120 42.0 / 48.0, one is as good or better.
+// Two tiles of outputs a wavefront where x is read for 33 - 48 tokens, from 1536 workgroups of one on.  us with one / two: six of 4096 of 4096, 40 tokens 26.1 / 24.6; three
+// of 8192 of 8192, 48 tokens 51.5 / 47.6; three of 4096 of 4096, 96 tokens 26.2 / 24.1; 13000 of 2048, 80 tokens, groups of 32 18.6 / 18.2; four of
+// 16384 of 4096, 130 tokens 164 / 156; two of 20480 of 5120, 70 tokens 85.7 / 86.3.  Below: 20480 of 5120, 40 tokens (1280) 29.7 / 27.8, but 8192 of 8192, 90 tokens, groups of
+// 32 (1024) 34.3 / 52.4.  Where x is read for 64 tokens, four of 8192 of 8192 69.6 / 71.8, and for 32, two of 20480 of 5120 42.0 / 48.0.
 template <int DT, int U, int NT>
 int32_t wide(W4Args &a, int64_t tiles, bool y16, void *stream)
 {
