@@ -55,3 +55,41 @@ def test_a_call_repeated_gives_the_same_bits(old, n, G, dtype):
             slora.kv8_attend(batch, 0, q.data_ptr(), width, out.data_ptr(), width, 0.125, True)  # without weights: the same outputs
             torch.cuda.synchronize()
             assert torch.equal(out, first[0])
+
+
+def test_a_graph_replays_prompts_and_evictions():
+    """what the other graph test leaves out: many columns and their weights, both forms of eviction (which give the same when repeated)"""
+    with Twin(1024, 64, 2, 4, "bf16", max_seqs=3, max_tokens=700) as t:
+        t.step([0, 1, 2], [500, 3, 600])
+        batch = t.step([0, 1], [70, 1])
+        few, some = t.plan([2], [0], [597]), t.plan([2], [0], [400])
+        width = t.kv * t.G * t.D
+        q, w = torch.zeros((71, width), dtype=t.dtype, device="cuda"), t.weight_arrays()
+        out, w2, p2 = torch.zeros_like(q), torch.zeros_like(w[0]), torch.zeros_like(w[2])
+        w[2][2] = torch.arange(700, device="cuda", dtype=torch.int32)
+
+        def call(stream):
+            slora.kv8_attend(batch, 0, q.data_ptr(), width, out.data_ptr(), width, 0.125, True, [x.data_ptr() for x in w], stream)
+            for b in (few, some):
+                slora.kv8_evict(b, 0, 20, w[0].data_ptr(), w2.data_ptr(), w[2].data_ptr(), p2.data_ptr(), stream)
+
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        call(stream)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call(torch.cuda.current_stream())
+        pool, exps = t.pool.clone(), t.exps.clone()
+        for _ in range(3):
+            q.copy_(torch.from_numpy(t.rng.standard_normal(q.shape)))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in (out, w[1], w2, p2)]
+            for x in (out, w2, p2):
+                x.zero_()
+            w[1].fill_(-1.0)
+            call(stream)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, (out, w[1], w2, p2)))
+            assert torch.equal(t.pool, pool) and torch.equal(t.exps, exps)

@@ -176,3 +176,13 @@ def test_queries_at_the_ends_of_bfloat16(power, n):
         t.step([0, 1], [60, 9])
         batch = t.step([0, 1], [n, n])
         attend_with_weights(t, batch, [0, 1], [n, n], size=2.0 ** power, scale=2.0 ** (-3 - power))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 12, 40])
+@pytest.mark.parametrize("scale", [-0.125, 0.0, -3.0])
+def test_scales_that_are_not_positive(n, scale, dtype):
+    with Twin(512, 64, 2, 2, dtype, max_seqs=2, max_tokens=300) as t:
+        t.step([0, 1], [200, 9])
+        batch = t.step([0, 1], [n, n])
+        attend_with_weights(t, batch, [0, 1], [n, n], scale=scale)
