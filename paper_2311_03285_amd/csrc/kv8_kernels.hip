@@ -197,8 +197,8 @@ __global__ __launch_bounds__(128) void kv_append_kernel(const KvItem *__restrict
 // half a percent where the cache's bytes are the bound (64 of 500 - 8000 tokens 123.9 us with one, 124.4 with two; 24 of 200 - 1500 60.0 / 60.4); for prompts to
 // the 11 bits of one, since two take a quarter longer (chunks of 128 - 1024 behind up to 4096 tokens 438 us / 539, a prompt of 512 29.5 / 31.6) and the output's own
 // rounding, to 11 or 8 bits, is as large.  p is taken 2^15 times as large (2^7 times for prompts, whose maximum may be 2^8 behind), the
-// largest power that stays in range, so that binary16 has its 11 bits down to 2^-29 (2^-21) of the largest.  The token whose s + u is m adds 2^-u >= 1 to it, so no sum is lost, whatever exponents there are: a token of equal score has
-// p >= 2^-100.  V of a block further below `top` is read in units of 2^(top - 100) instead of its own, which puts its elements off by less than 2^(top - 93).
+// largest power that stays in range, so that binary16 has its 11 bits down to 2^-29 (2^-21) of the largest.
+// The token whose s + u is m adds 2^-u >= 1 to the scores' sum, and one of equal score has p >= 2^-100, whatever exponents there are.  V of a block further below `top` is read in units of 2^(top - 100) instead of its own, which puts its elements off by less than 2^(top - 93).
 // A block with an infinity or NaN in V has u = 0, and the columns that see any of its tokens - their limits are behind its first one - get NaN at the end: the
 // scores' sum, which the weights are taken from, knows nothing of V.
 __device__ __forceinline__ f32x4 mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
