@@ -510,6 +510,85 @@ int32_t slora_w4_destroy(slora_w4 *w);
 int32_t slora_w4_matmul(int32_t n, const slora_w4 *const *w, const void *const *x, int32_t T, float *const *y, void *stream);
 int32_t slora_w4_matmul_y16(int32_t n, const slora_w4 *const *w, const void *const *x, int32_t T, void *const *y, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The dense side of a layer in 8-bit integers: norms around a block with its gate and residual, rows in 8 bits, and products of
+ * 8-bit x with 8-bit weights - the base model's xW (Fig. 1) of prompts and of decode batches alike.
+ *
+ * A row v in 8 bits is its codes and one fp32 scale: with a = max(max |v|, 2^-100),
+ *   scale = a / 127,  code = v * (127 / a) rounded to nearest, ties to even (-127 .. 127);  v is about code * scale.
+ * Quotients and product are fp32.  A row that holds an infinity or a NaN has codes 0 and a NaN for its scale, so that
+ * its products are NaN.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct slora_norm slora_norm;
+typedef struct slora_w8 slora_w8;
+
+/*
+ * A junction of two blocks: the norm behind one (optional), its gate and residual scale, and the norm before the next.
+ *   b' = N(b; post_weight, post_bias) with SLORA_NORM_POST, else b
+ *   h' = h + scale * gate * b'
+ *   x  = N(h'; pre_weight, pre_bias)
+ *   N(v; w, c) = v / sqrt(mean(v^2) + eps) * w + c, or with SLORA_NORM_LAYER (v - mean(v)) / sqrt(var(v) + eps) * w + c
+ * post_weight .. pre_bias: DEVICE vectors of `width` elements of `dtype`, 16-byte aligned, borrowed until slora_norm_destroy; a weight that is NULL
+ * is 1, a bias that is NULL 0 (post ones without SLORA_NORM_POST: EINVAL).  1 <= width <= SLORA_NORM_MAX_WIDTH;
+ * eps: 0, or at least 2^-60; scale finite.  SLORA_NORM_H32: the residual stream h is fp32, otherwise of `dtype`.
+ * The junction belongs to the HIP device that is current.
+ */
+enum { SLORA_NORM_LAYER = 1, SLORA_NORM_POST = 2, SLORA_NORM_H32 = 4 };
+#define SLORA_NORM_MAX_WIDTH 32768
+int32_t slora_norm_init(slora_norm **out, int32_t width, int32_t dtype, int32_t flags, float eps, float scale, const void *post_weight,
+                        const void *post_bias, const void *pre_weight, const void *pre_bias);
+int32_t slora_norm_destroy(slora_norm *norm);
+
+/*
+ * One pass over T tokens.  All of it is DEVICE memory; row t of an array begins at t * its stride, in elements.
+ * h; h_out: h', rounded once; NULL: not wanted.
+ * block: b, of `dtype`; NULL: h' = h (gate has to be NULL).  gate: of `dtype`, a row for each token, or with gate_stride 0 one for all; NULL: 1.
+ * x: of `dtype`; codes, scales: x in 8 bits, of the fp32 values that x is rounded from; NULL (scales with codes): not wanted.
+ * Norms are of h' before it is rounded; sums are fp32.  16-byte aligned, strides multiples of 8 (codes: of 16) and at
+ * least `width`; nothing behind a row's `width` elements is read or written.  h_out may be h, x may be block, of equal strides; no other arrays
+ * may overlap.  Tokens do not affect each other; results do not depend on T.  Allocates nothing; may be captured in a HIP graph.
+ */
+int32_t slora_norm_apply(const slora_norm *norm, int32_t T, const void *h, int64_t h_stride, const void *block, int64_t block_stride, const void *gate,
+                         int64_t gate_stride, void *h_out, int64_t h_out_stride, void *x, int64_t x_stride, int8_t *codes, int64_t codes_stride,
+                         float *scales, void *stream);
+
+/*
+ * T rows of v = x (act == SLORA_ACT_NONE, gate NULL), or v = act(gate) * x, in 16 bits (y), in 8 bits (codes, scales), or both; what is NULL is not
+ * wanted.  silu(g) = g / (1 + exp(-g)); gelu(g) = g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2.  x, gate, y: of `dtype`.
+ * 1 <= width <= SLORA_W8_MAX_WIDTH.  Arrays, strides, overlaps (y may be x or gate), asynchrony as for slora_norm_apply.
+ * Runs on the HIP device that is current.
+ */
+enum { SLORA_ACT_NONE = 0, SLORA_ACT_SILU = 1, SLORA_ACT_GELU = 2 };
+#define SLORA_W8_MAX_WIDTH 65536
+int32_t slora_w8_quantize(int32_t T, int32_t width, int32_t dtype, int32_t act, const void *x, int64_t x_stride, const void *gate, int64_t gate_stride,
+                          void *y, int64_t y_stride, int8_t *codes, int64_t codes_stride, float *scales, void *stream);
+
+/*
+ * Lay out one matrix for the product.  codes: DEVICE [outputs][inputs]; scales: DEVICE [outputs], fp32, 4-byte aligned.
+ * 1 <= inputs <= SLORA_W8_MAX_INPUTS, which sums of products of any codes fit in 32 bits, 1 <= outputs <= 2^24.  packed: DEVICE, slora_w8_bytes(...)
+ * bytes, 16-byte aligned, borrowed until slora_w8_destroy; it is written by a kernel on `stream`, after which codes and scales are no
+ * longer needed.  dtype: the 16-bit type of y.  The matrix belongs to the HIP device that is current.
+ */
+#define SLORA_W8_MAX_INPUTS 131071
+int32_t slora_w8_bytes(int32_t outputs, int32_t inputs, int64_t *out);
+int32_t slora_w8_pack(slora_w8 **out, int32_t outputs, int32_t inputs, int32_t dtype, const int8_t *codes, const float *scales, void *packed,
+                      void *stream);
+int32_t slora_w8_destroy(slora_w8 *w);
+
+/*
+ * y[k][t, o] = (sum_i x[k][t, i] * codes_k[o, i]) * x_scales[k][t] * scales_k[o] for n <= SLORA_MAX_MULTI matrices in one launch.
+ * x[k]: DEVICE, T rows of w[k]'s inputs, 16-byte aligned, x_stride[k] bytes apart: a multiple of 16, at least inputs, at most 2^22; bytes up to
+ * the next multiple of 16 behind a row are read and may hold anything.  x_scales[k]: DEVICE, T fp32, 4-byte aligned.  Entries of x and of x_scales may be equal.
+ * y[k]: DEVICE, 16-byte aligned, T rows of w[k]'s outputs, y_stride[k] >= outputs elements apart, fp32 or (_y16) of its 16-bit type,
+ * written, not added to; nothing behind a row is written, and entries must not overlap.  x_stride, y_stride: HOST arrays.
+ * Sums are whole numbers in 32 bits, exact in any order; each is rounded to fp32, multiplied by both scales there, and
+ * rounded to y's type.  All matrices have one type and one device.  Allocates nothing; may be captured in a HIP graph.
+ */
+int32_t slora_w8_matmul(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales,
+                        int32_t T, float *const *y, const int64_t *y_stride, void *stream);
+int32_t slora_w8_matmul_y16(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales,
+                            int32_t T, void *const *y, const int64_t *y_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

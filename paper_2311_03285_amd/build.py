@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslora_hip.so")
-SOURCES = ["pool.cpp", "plan.cpp", "kernels.hip", "kv8.cpp", "kv8_kernels.hip", "w4.cpp", "w4_kernels.hip"]
+SOURCES = ["pool.cpp", "plan.cpp", "kernels.hip", "kv8.cpp", "kv8_kernels.hip", "w4.cpp", "w4_kernels.hip", "rows.cpp", "rows_kernels.hip", "w8.cpp",
+           "w8_kernels.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,0 +1,506 @@
+// gfx950 kernels on whole rows: norms around a block with its gate and residual, rows in 8 bits.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_device.hpp"
+#include "rows.hpp"
+
+namespace slora {
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------------------
+// a row in registers
+// ---------------------------------------------------------------------------------------
+// A row belongs to `waves` wavefronts and stays in their registers from its one load to its stores.  Its whole pieces of eight
+// elements are dealt out in turn, P to a lane at most; the elements behind the last whole piece (TAIL) are one more piece of the row's last lane, read and
+// written element by element, so that nothing behind the row is touched.
+// Loads are not behind branches: a lane without a piece reads the row's last one once more.
+template <int P, bool TAIL>
+struct Row {
+    static constexpr int kParts = P + (TAIL ? 1 : 0);
+    int lane, lanes; // of the row
+    int pieces, rest; // whole pieces, elements behind them
+    __device__ __forceinline__ bool has(int p) const { return p < P ? lane + p * lanes < pieces : lane == lanes - 1; }
+    __device__ __forceinline__ int at(int p) const { return (p < P ? min(lane + p * lanes, max(pieces - 1, 0)) : pieces) * kPiece; }
+    __device__ __forceinline__ bool valid(int p, int i) const { return has(p) && (p < P || i < rest); }
+};
+
+template <int DT>
+__device__ __forceinline__ void widen8(const u32x4 &raw, float (&v)[kPiece])
+{
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) v[i] = widen<DT>((uint16_t)(raw[i / 2] >> (16 * (i % 2))));
+}
+
+// a 16-bit vector's pieces as they are
+template <int P, bool TAIL>
+__device__ __forceinline__ void load16(const Row<P, TAIL> &r, const uint16_t *from, u32x4 (&raw)[Row<P, TAIL>::kParts])
+{
+    if (!TAIL || r.pieces > 0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) raw[p] = *reinterpret_cast<const u32x4 *>(from + r.at(p));
+    }
+    if constexpr (TAIL) {
+        uint16_t e[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) e[i] = from[r.at(P) + min(i, r.rest - 1)];
+#pragma unroll
+        for (int i = 0; i < kPiece / 2; ++i) raw[P][i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+    }
+}
+template <int P, bool TAIL>
+__device__ __forceinline__ void load32(const Row<P, TAIL> &r, const float *from, f32x4 (&raw)[Row<P, TAIL>::kParts][2])
+{
+    if (!TAIL || r.pieces > 0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) raw[p][i] = *reinterpret_cast<const f32x4 *>(from + r.at(p) + 4 * i);
+    }
+    if constexpr (TAIL) {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) raw[P][i / 4][i % 4] = from[r.at(P) + min(i, r.rest - 1)];
+    }
+}
+template <int DT, int P, bool TAIL>
+__device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, const float (&v)[Row<P, TAIL>::kParts][kPiece])
+{
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+        if (!r.has(p)) continue;
+        uint16_t e[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) e[i] = narrow<DT>(v[p][i]);
+        if (p < P) {
+            u32x4 u;
+#pragma unroll
+            for (int i = 0; i < kPiece / 2; ++i) u[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+            *reinterpret_cast<u32x4 *>(to + r.at(p)) = u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPiece - 1; ++i)
+                if (i < r.rest) to[r.at(p) + i] = e[i];
+        }
+    }
+}
+template <int P, bool TAIL>
+__device__ __forceinline__ void store32(const Row<P, TAIL> &r, float *to, const float (&v)[Row<P, TAIL>::kParts][kPiece])
+{
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+        if (!r.has(p)) continue;
+        if (p < P) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4 *>(to + r.at(p) + 4 * i) = f32x4{v[p][4 * i], v[p][4 * i + 1], v[p][4 * i + 2], v[p][4 * i + 3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPiece - 1; ++i)
+                if (i < r.rest) to[r.at(p) + i] = v[p][i];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// sums and maxima over a row
+// ---------------------------------------------------------------------------------------
+// over the wavefront, without LDS: lanes of 16 by shifts, then what the 16s before have found; the total is the last lane's
+__device__ __forceinline__ float wave_sum(float v)
+{
+#define SLORA_STEP(control, rows) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), control, rows, 0xf, false))
+    SLORA_STEP(0x111, 0xf); // row_shr 1, 2, 4, 8
+    SLORA_STEP(0x112, 0xf);
+    SLORA_STEP(0x114, 0xf);
+    SLORA_STEP(0x118, 0xf);
+    SLORA_STEP(0x142, 0xa); // row_bcast 15, 31
+    SLORA_STEP(0x143, 0xc);
+#undef SLORA_STEP
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+__device__ __forceinline__ int wave_max(int v)
+{
+#define SLORA_STEP(control) v = max(v, __builtin_amdgcn_update_dpp(v, v, control, 0xf, 0xf, false))
+    SLORA_STEP(0x111);
+    SLORA_STEP(0x112);
+    SLORA_STEP(0x114);
+    SLORA_STEP(0x118);
+    SLORA_STEP(0x142);
+    SLORA_STEP(0x143);
+#undef SLORA_STEP
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Over the row's wavefronts, in their order.  Each reduction has words of its own, so one barrier does.
+struct Team {
+    uint32_t (*slots)[kRowThreads / kWave];
+    int waves, wave, used = 0;
+    __device__ __forceinline__ float sum(float v)
+    {
+        v = wave_sum(v);
+        if (waves == 1) return v;
+        uint32_t *s = slots[used++];
+        if (threadIdx.x % kWave == 0) s[wave] = __float_as_uint(v);
+        __syncthreads();
+        v = 0.0f;
+        for (int w = 0; w < waves; ++w) v += __uint_as_float(s[w]);
+        return v;
+    }
+    __device__ __forceinline__ int max_of(int v)
+    {
+        v = wave_max(v);
+        if (waves == 1) return v;
+        uint32_t *s = slots[used++];
+        if (threadIdx.x % kWave == 0) s[wave] = (uint32_t)v;
+        __syncthreads();
+        v = 0;
+        for (int w = 0; w < waves; ++w) v = max(v, (int)s[w]);
+        return v;
+    }
+};
+constexpr int kReductions = 11; // most of a row: two norms of five (mean, spread, maximum, mean, spread) and the codes' maximum
+
+// bits of a magnitude: in the order of the numbers, NaN above infinity
+__device__ __forceinline__ int magnitude(float v) { return (int)(__float_as_uint(v) & 0x7fffffffu); }
+
+template <int P, bool TAIL>
+__device__ __forceinline__ int largest(const Row<P, TAIL> &r, const float (&v)[Row<P, TAIL>::kParts][kPiece], Team &team)
+{
+    int top = 0;
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) top = max(top, r.valid(p, i) ? magnitude(v[p][i]) : 0);
+    return team.max_of(top);
+}
+
+// ---------------------------------------------------------------------------------------
+// norms
+// ---------------------------------------------------------------------------------------
+struct Spread {
+    float mean, square; // square: mean square of v - mean
+};
+template <int P, bool TAIL>
+__device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (&v)[Row<P, TAIL>::kParts][kPiece], bool layer, int width, Team &team)
+{
+    Spread s{0.0f, 0.0f};
+    if (layer) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) sum += r.valid(p, i) ? v[p][i] : 0.0f;
+        s.mean = team.sum(sum) / (float)width;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            const float d = r.valid(p, i) ? v[p][i] - s.mean : 0.0f;
+            sum = __builtin_fmaf(d, d, sum);
+        }
+    s.square = team.sum(sum) / (float)width;
+    return s;
+}
+
+// v = (v - mean) / sqrt(mean square + eps), with all of the row in registers: the spread is of differences, not a difference of sums.
+// Squares that leave fp32's range (bfloat16 and fp32 rows can) are taken again of v times a power of two, which is
+// exact; eps, which is 0 or at least 2^-60, is then 0 or negligible or scaled along.  All lanes of the row go the same way.
+template <int P, bool TAIL>
+__device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[Row<P, TAIL>::kParts][kPiece], bool layer, int width, float eps, Team &team)
+{
+    Spread s = spread_of(r, v, layer, width, team);
+    float q = s.square + eps;
+    if (!(q >= 0x1p-80f && q <= 0x1p100f)) {
+        const int top = largest(r, v, team);
+        if (top < 0x7f800000) { // (an infinity or NaN spoils its row either way)
+            // the largest magnitude to about 1: factors 2^up, two of them where one is no normal number
+            const int up = 127 - max(top >> 23, 1);
+            const float a = __uint_as_float((uint32_t)(127 + up / 2) << 23), b = __uint_as_float((uint32_t)(127 + (up - up / 2)) << 23);
+#pragma unroll
+            for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) v[p][i] = v[p][i] * a * b;
+            s = spread_of(r, v, layer, width, team);
+            q = s.square + eps * a * b * a * b;
+        }
+    }
+    const float by = 1.0f / sqrtf(q);
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[p][i] = (v[p][i] - s.mean) * by;
+}
+
+// v = v * weight + bias, where there are any
+template <int DT, int P, bool TAIL>
+__device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[Row<P, TAIL>::kParts][kPiece], const u32x4 (&weight)[Row<P, TAIL>::kParts], const uint16_t *w,
+                                       const uint16_t *bias)
+{
+    if (w) {
+#pragma unroll
+        for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+            float e[kPiece];
+            widen8<DT>(weight[p], e);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) v[p][i] *= e[i];
+        }
+    }
+    if (bias) {
+        u32x4 raw[Row<P, TAIL>::kParts];
+        load16(r, bias, raw);
+#pragma unroll
+        for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+            float e[kPiece];
+            widen8<DT>(raw[p], e);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) v[p][i] += e[i];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// 8 bits
+// ---------------------------------------------------------------------------------------
+// Codes are rounded from fp32 values (not from the 16 bits that x is rounded to: one rounding, not two).
+template <int P, bool TAIL>
+__device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut &out, int64_t t, const float (&v)[Row<P, TAIL>::kParts][kPiece], Team &team)
+{
+    const int top = largest(r, v, team);
+    const bool spoiled = top >= 0x7f800000;
+    const float a = fmaxf(__uint_as_float((uint32_t)top), kW8Least), inverse = spoiled ? 0.0f : 127.0f / a;
+    int8_t *to = out.codes + t * out.codes_stride;
+#pragma unroll
+    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+        if (!r.has(p)) continue;
+        uint32_t c[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) c[i] = spoiled ? 0u : (uint32_t)(int)__builtin_rintf(v[p][i] * inverse) & 0xffu;
+        if (p < P) {
+            u32x2 u;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) u[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | c[4 * i + 3] << 24;
+            *reinterpret_cast<u32x2 *>(to + r.at(p)) = u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPiece - 1; ++i)
+                if (i < r.rest) to[r.at(p) + i] = (int8_t)c[i];
+        }
+    }
+    if (r.lane == 0) out.scales[t] = spoiled ? __uint_as_float(0x7fc00000u) : a / 127.0f;
+}
+
+constexpr int kGridX = 1 << 20; // workgroups along x: with 1024 threads each they stay below 2^32 threads
+
+template <int P, bool TAIL>
+__device__ __forceinline__ Row<P, TAIL> row_of(int width, int waves)
+{
+    Row<P, TAIL> r;
+    r.lanes = waves * kWave;
+    r.lane = waves == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
+    r.pieces = width / kPiece;
+    r.rest = width % kPiece;
+    return r;
+}
+
+__device__ __forceinline__ int64_t row_number(int waves, int wave)
+{
+    const int64_t block = (int64_t)blockIdx.y * kGridX + blockIdx.x;
+    return waves == 1 ? block * (blockDim.x / kWave) + wave : block;
+}
+
+// One row for the workgroup, or (waves == 1) one for each of its wavefronts.
+// Bound: HBM.
+template <int DT, bool H32, int P, bool TAIL>
+__global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves)
+{
+    constexpr int kParts = Row<P, TAIL>::kParts;
+    __shared__ uint32_t slots[kReductions][kRowThreads / kWave];
+    const int wave = wave_number();
+    const int64_t t = row_number(waves, wave);
+    if (t >= a.T) return; // (all wavefronts that share barriers)
+    const Row<P, TAIL> r = row_of<P, TAIL>(a.width, waves);
+    Team team{slots, waves, wave};
+
+    // With four pieces a lane there are no registers for what is not needed yet: 128 of them, where a workgroup may have 16 wavefronts.
+    constexpr bool kAhead = P <= 2;
+    auto not_before = [] {
+        if constexpr (!kAhead) asm volatile("" ::: "memory");
+    };
+    float v[kParts][kPiece];
+    typedef typename std::conditional<H32, f32x4[kParts][2], u32x4[kParts]>::type Raw;
+    Raw h;
+    auto load_h = [&] {
+        if constexpr (H32)
+            load32(r, static_cast<const float *>(a.h) + t * a.h_stride, h);
+        else
+            load16(r, static_cast<const uint16_t *>(a.h) + t * a.h_stride, h);
+    };
+    if constexpr (kAhead) load_h();
+    if (a.block) {
+        u32x4 raw[kParts], weight[kParts], gate[kParts];
+        auto load_weight = [&] {
+            if (a.post && a.post_weight) load16(r, a.post_weight, weight);
+        };
+        auto load_gate = [&] {
+            if (a.gate) load16(r, a.gate + t * a.gate_stride, gate);
+        };
+        load16(r, a.block + t * a.block_stride, raw);
+        if constexpr (kAhead) load_weight();
+        if constexpr (kAhead) load_gate();
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) widen8<DT>(raw[p], v[p]);
+        if (a.post) {
+            normalise(r, v, a.layer != 0, a.width, a.eps, team);
+            not_before();
+            if constexpr (!kAhead) load_weight();
+            affine<DT>(r, v, weight, a.post_weight, a.post_bias);
+        }
+        not_before();
+        if constexpr (!kAhead) load_gate();
+        if (a.gate) {
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                float e[kPiece];
+                widen8<DT>(gate[p], e);
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) v[p][i] *= e[i];
+            }
+        }
+    }
+    not_before();
+    if constexpr (!kAhead) load_h();
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+        float e[kPiece];
+        if constexpr (H32) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) e[i] = h[p][i / 4][i % 4];
+        } else {
+            widen8<DT>(h[p], e);
+        }
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[p][i] = a.block ? __builtin_fmaf(a.scale, v[p][i], e[i]) : e[i];
+    }
+    if (a.h_out) {
+        if constexpr (H32)
+            store32(r, static_cast<float *>(a.h_out) + t * a.h_out_stride, v);
+        else
+            store16<DT>(r, static_cast<uint16_t *>(a.h_out) + t * a.h_out_stride, v);
+    }
+    if (!a.out.x && !a.out.codes) return;
+    u32x4 weight[kParts];
+    auto load_weight = [&] {
+        if (a.pre_weight) load16(r, a.pre_weight, weight);
+    };
+    if constexpr (kAhead) load_weight();
+    normalise(r, v, a.layer != 0, a.width, a.eps, team);
+    not_before();
+    if constexpr (!kAhead) load_weight();
+    affine<DT>(r, v, weight, a.pre_weight, a.pre_bias);
+    if (a.out.x) store16<DT>(r, a.out.x + t * a.out.x_stride, v);
+    if (a.out.codes) store_codes(r, a.out, t, v, team);
+}
+
+// ... as above
+template <int DT, int P, bool TAIL>
+__global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, int waves)
+{
+    constexpr int kParts = Row<P, TAIL>::kParts;
+    __shared__ uint32_t slots[1][kRowThreads / kWave];
+    const int wave = wave_number();
+    const int64_t t = row_number(waves, wave);
+    if (t >= a.T) return;
+    const Row<P, TAIL> r = row_of<P, TAIL>(a.width, waves);
+    Team team{slots, waves, wave};
+    u32x4 raw[kParts], gate[kParts];
+    load16(r, a.x + t * a.x_stride, raw);
+    if (a.gate) load16(r, a.gate + t * a.gate_stride, gate);
+    float v[kParts][kPiece];
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+        widen8<DT>(raw[p], v[p]);
+        if (a.gate) {
+            float g[kPiece];
+            widen8<DT>(gate[p], g);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) {
+                // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+                const float u = a.act == SLORA_ACT_SILU ? g[i] : 1.5957691216057308f * __builtin_fmaf(0.044715f * g[i] * g[i], g[i], g[i]);
+                v[p][i] *= g[i] / (1.0f + expf(-u));
+            }
+        }
+    }
+    if (a.out.x) store16<DT>(r, a.out.x + t * a.out.x_stride, v);
+    if (a.out.codes) store_codes(r, a.out, t, v, team);
+}
+
+// f(pieces of a lane, wavefronts of a row)
+template <int MOST, typename F>
+int32_t by_width(int width, F f)
+{
+    const int pieces = std::max(width / kPiece, 1);
+    auto waves = [&](int p) { return (pieces + p * kWave - 1) / (p * kWave); };
+    if (waves(1) <= 1) return f(std::integral_constant<int, 1>{}, 1);
+    if (waves(2) <= 16) return f(std::integral_constant<int, 2>{}, waves(2));
+    if constexpr (MOST == 8) {
+        if (waves(4) > 16) return f(std::integral_constant<int, 8>{}, waves(8));
+    }
+    return f(std::integral_constant<int, 4>{}, waves(4));
+}
+
+// rows of one wavefront: four to a workgroup
+struct Grid {
+    dim3 blocks, threads;
+    Grid(int32_t T, int waves) : threads(waves == 1 ? 4 * kWave : waves * kWave)
+    {
+        const int64_t n = waves == 1 ? ((int64_t)T + 3) / 4 : T;
+        blocks = dim3((unsigned)std::min<int64_t>(n, kGridX), (unsigned)((n + kGridX - 1) / kGridX));
+    }
+};
+
+template <typename F>
+int32_t by_flag(bool flag, F f)
+{
+    return flag ? f(std::true_type{}) : f(std::false_type{});
+}
+
+} // namespace
+
+int32_t launch_norm(const NormArgs &a, int32_t dtype, bool h32, void *stream)
+{
+    return by_width<4>(a.width, [&](auto p, int waves) {
+        return by_flag(a.width % kPiece != 0, [&](auto tail) {
+            return by_flag(h32, [&](auto h) {
+                const Grid g(a.T, waves);
+                if (dtype == SLORA_F16)
+                    hipLaunchKernelGGL((norm_kernel<SLORA_F16, h.value, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                else
+                    hipLaunchKernelGGL((norm_kernel<SLORA_BF16, h.value, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                return check_launch("norm");
+            });
+        });
+    });
+}
+
+int32_t launch_quantize(const QuantizeArgs &a, int32_t dtype, void *stream)
+{
+    return by_width<8>(a.width, [&](auto p, int waves) {
+        return by_flag(a.width % kPiece != 0, [&](auto tail) {
+            const Grid g(a.T, waves);
+            if (dtype == SLORA_F16)
+                hipLaunchKernelGGL((quantize_kernel<SLORA_F16, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+            else
+                hipLaunchKernelGGL((quantize_kernel<SLORA_BF16, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+            return check_launch("quantize");
+        });
+    });
+}
+
+} // namespace slora

@@ -1,0 +1,138 @@
+// Products with 8-bit weights: checks of the arguments.
+#include <hip/hip_runtime_api.h>
+
+#include <new>
+
+#include "w8.hpp"
+
+using namespace slora;
+
+namespace {
+
+int32_t check_shape(int32_t outputs, int32_t inputs)
+{
+    if (outputs < 1 || outputs > 1 << 24) return fail(SLORA_EINVAL, "outputs=%d must be in [1, 2^24]", outputs);
+    if (inputs < 1 || inputs > SLORA_W8_MAX_INPUTS) return fail(SLORA_EINVAL, "inputs=%d must be in [1, %d]", inputs, SLORA_W8_MAX_INPUTS);
+    return SLORA_OK;
+}
+
+void shape(slora_w8 &w, int32_t outputs, int32_t inputs)
+{
+    w.outputs = outputs;
+    w.inputs = inputs;
+    w.tiles = (outputs + kW8Rows - 1) / kW8Rows;
+    w.chunks = (inputs + 2 * kW8Chunk - 1) / (2 * kW8Chunk) * 2;
+}
+
+} // namespace
+
+extern "C" {
+
+int32_t slora_w8_bytes(int32_t outputs, int32_t inputs, int64_t *out)
+{
+    clear_error();
+    if (!out) return fail(SLORA_EINVAL, "out is NULL");
+    int32_t rc = check_shape(outputs, inputs);
+    if (rc != SLORA_OK) return rc;
+    slora_w8 w;
+    shape(w, outputs, inputs);
+    *out = w.code_bytes() + (int64_t)w.tiles * kW8Rows * 4;
+    return SLORA_OK;
+}
+
+int32_t slora_w8_pack(slora_w8 **out, int32_t outputs, int32_t inputs, int32_t dtype, const int8_t *codes, const float *scales, void *packed,
+                      void *stream)
+{
+    clear_error();
+    if (!out) return fail(SLORA_EINVAL, "out is NULL");
+    *out = nullptr;
+    int32_t rc = check_shape(outputs, inputs);
+    if (rc != SLORA_OK) return rc;
+    if (dtype != SLORA_F16 && dtype != SLORA_BF16) return fail(SLORA_EINVAL, "unknown dtype %d", dtype);
+    if (!codes || !scales || !packed) return fail(SLORA_EINVAL, "codes, scales and packed are needed");
+    if (reinterpret_cast<uintptr_t>(packed) & 15) return fail(SLORA_EINVAL, "packed must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(scales) & 3) return fail(SLORA_EINVAL, "scales must be 4-byte aligned");
+    slora_w8 *w = new (std::nothrow) slora_w8;
+    if (!w) return fail(SLORA_ENOMEM, "out of host memory");
+    shape(*w, outputs, inputs);
+    w->dtype = dtype;
+    w->packed = static_cast<const int8_t *>(packed);
+    const hipError_t e = hipGetDevice(&w->device);
+    rc = e == hipSuccess ? launch_w8_pack(w, codes, scales, packed, stream) : fail(SLORA_EHIP, "hipGetDevice: %s", hipGetErrorString(e));
+    if (rc != SLORA_OK) {
+        delete w;
+        return rc;
+    }
+    *out = w;
+    return SLORA_OK;
+}
+
+int32_t slora_w8_destroy(slora_w8 *w)
+{
+    clear_error();
+    delete w;
+    return SLORA_OK;
+}
+
+} // extern "C"
+
+namespace {
+int32_t matmul(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales, int32_t T, void *const *y,
+               const int64_t *y_stride, bool y16, void *stream)
+{
+    clear_error();
+    if (n < 1 || n > SLORA_MAX_MULTI) return fail(SLORA_EINVAL, "n=%d must be in [1, %d]", n, SLORA_MAX_MULTI);
+    if (!w || !x || !x_stride || !x_scales || !y || !y_stride) return fail(SLORA_EINVAL, "NULL argument");
+    if (T < 0) return fail(SLORA_EINVAL, "T=%d is negative", T);
+    if (T > 1 << 30) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", T); // (32-bit numbers of tokens, tiles' ends included)
+    W8Args a{};
+    a.n = n;
+    a.T = T;
+    for (int32_t k = 0; k < n; ++k) {
+        if (!w[k]) return fail(SLORA_EINVAL, "w[%d] is NULL", k);
+        if (w[k]->dtype != w[0]->dtype || w[k]->device != w[0]->device) return fail(SLORA_EINVAL, "w[%d] has another type or device than w[0]", k);
+        if (T == 0) continue;
+        if (!x[k] || !x_scales[k] || !y[k]) return fail(SLORA_EINVAL, "x[%d], x_scales[%d] or y[%d] is NULL", k, k, k);
+        if ((reinterpret_cast<uintptr_t>(x[k]) | reinterpret_cast<uintptr_t>(y[k])) & 15) return fail(SLORA_EINVAL, "x[%d] and y[%d] must be 16-byte aligned", k, k);
+        if (reinterpret_cast<uintptr_t>(x_scales[k]) & 3) return fail(SLORA_EINVAL, "x_scales[%d] must be 4-byte aligned", k);
+        if (x_stride[k] < w[k]->inputs || x_stride[k] % 16 || x_stride[k] > kW8MostStride)
+            return fail(SLORA_EINVAL, "x_stride[%d]=%lld must be a multiple of 16, at least %d and at most 2^22", k, (long long)x_stride[k], w[k]->inputs);
+        if (y_stride[k] < w[k]->outputs || y_stride[k] > int64_t(1) << 29)
+            return fail(SLORA_EINVAL, "y_stride[%d]=%lld must be at least %d and at most 2^29", k, (long long)y_stride[k], w[k]->outputs);
+        for (int32_t m = 0; m < k; ++m)
+            if (y[m] == y[k]) return fail(SLORA_EINVAL, "y[%d] and y[%d] are the same buffer", m, k);
+        W8Matrix &to = a.m[k];
+        to.codes = w[k]->packed;
+        to.scales = w[k]->scales();
+        to.x = x[k];
+        to.x_scales = x_scales[k];
+        to.y = y[k];
+        to.y_stride = y_stride[k];
+        to.outputs = w[k]->outputs;
+        to.chunks = w[k]->chunks;
+        to.tiles = w[k]->tiles;
+        to.x_stride = (int32_t)x_stride[k];
+        to.x_last = (w[k]->inputs - 1) / 16 * 16;
+    }
+    if (T == 0) return SLORA_OK;
+    DeviceScope dev(w[0]->device);
+    if (dev.status() != SLORA_OK) return dev.status();
+    return launch_w8(a, y16 ? 1 + w[0]->dtype : 0, stream);
+}
+} // namespace
+
+extern "C" {
+
+int32_t slora_w8_matmul(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales, int32_t T,
+                        float *const *y, const int64_t *y_stride, void *stream)
+{
+    return matmul(n, w, x, x_stride, x_scales, T, reinterpret_cast<void *const *>(y), y_stride, false, stream);
+}
+
+int32_t slora_w8_matmul_y16(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales, int32_t T,
+                            void *const *y, const int64_t *y_stride, void *stream)
+{
+    return matmul(n, w, x, x_stride, x_scales, T, y, y_stride, true, stream);
+}
+
+} // extern "C"

@@ -20,6 +20,8 @@ STATIC_SCRATCH_BYTES = 64 << 20
 PLAN_INFO_N = 13
 POOL_STATS_N = 4
 KV8_INFO_N = 4
+NORM_LAYER, NORM_POST, NORM_H32 = 1, 2, 4
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
 PLAN_INFO_KEYS = ("tokens", "groups", "groups_vec", "groups_mfma", "vec_shrink_items", "vec_expand_items",
                   "mfma_shrink_items", "mfma_expand_items", "v_stride", "sum_rank", "split_tiles",
                   "scratch_bytes_per_slot", "groups_fused")
@@ -91,6 +93,15 @@ def lib() -> C.CDLL:
             "slora_w4_destroy": (i32, [vp]),
             "slora_w4_matmul": (i32, [i32, vp, vp, i32, vp, vp]),
             "slora_w4_matmul_y16": (i32, [i32, vp, vp, i32, vp, vp]),
+            "slora_norm_init": (i32, [C.POINTER(vp), i32, i32, i32, C.c_float, C.c_float, vp, vp, vp, vp]),
+            "slora_norm_destroy": (i32, [vp]),
+            "slora_norm_apply": (i32, [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+            "slora_w8_quantize": (i32, [i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+            "slora_w8_bytes": (i32, [i32, i32, vp]),
+            "slora_w8_pack": (i32, [C.POINTER(vp), i32, i32, i32, vp, vp, vp, vp]),
+            "slora_w8_destroy": (i32, [vp]),
+            "slora_w8_matmul": (i32, [i32, vp, vp, vp, vp, i32, vp, vp, vp]),
+            "slora_w8_matmul_y16": (i32, [i32, vp, vp, vp, vp, i32, vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -409,3 +420,70 @@ def w4_matmul_y16(handles, xs: Sequence[int], T: int, ys: Sequence[int], stream=
     if not len(handles) == len(xs) == len(ys):
         raise ValueError("as many xs and ys as matrices")
     _check(lib().slora_w4_matmul_y16(len(handles), _handle_array(handles), _ptr_array(xs), T, _ptr_array(ys), _stream(stream)))
+
+
+# ---- norms around a block, rows in 8 bits, products with 8-bit weights -----------------------------
+def norm_init(width: int, dtype: int, flags: int = 0, eps: float = 1e-5, scale: float = 1.0, post_weight: Optional[int] = None,
+              post_bias: Optional[int] = None, pre_weight: Optional[int] = None, pre_bias: Optional[int] = None) -> C.c_void_p:
+    """Device addresses of vectors of `width` elements, borrowed until norm_destroy; flags: NORM_LAYER | NORM_POST | NORM_H32."""
+    h = C.c_void_p()
+    _check(lib().slora_norm_init(C.byref(h), width, dtype, flags, eps, scale, post_weight or None, post_bias or None, pre_weight or None, pre_bias or None))
+    return h
+
+
+def norm_destroy(norm) -> None:
+    _check(lib().slora_norm_destroy(norm))
+
+
+def norm_apply(norm, T: int, h: int, h_stride: int, block: Optional[int] = None, block_stride: int = 0, gate: Optional[int] = None, gate_stride: int = 0,
+               h_out: Optional[int] = None, h_out_stride: int = 0, x: Optional[int] = None, x_stride: int = 0, codes: Optional[int] = None,
+               codes_stride: int = 0, scales: Optional[int] = None, stream=None) -> None:
+    """Device addresses; strides between rows in elements."""
+    _check(lib().slora_norm_apply(norm, T, h or None, h_stride, block or None, block_stride, gate or None, gate_stride, h_out or None, h_out_stride,
+                                  x or None, x_stride, codes or None, codes_stride, scales or None, _stream(stream)))
+
+
+def w8_quantize(T: int, width: int, dtype: int, act: int, x: int, x_stride: int, gate: Optional[int] = None, gate_stride: int = 0, y: Optional[int] = None,
+                y_stride: int = 0, codes: Optional[int] = None, codes_stride: int = 0, scales: Optional[int] = None, stream=None) -> None:
+    """Rows of x, or of act(gate) * x, in 16 bits (y), in 8 bits (codes, scales), or both."""
+    _check(lib().slora_w8_quantize(T, width, dtype, act, x or None, x_stride, gate or None, gate_stride, y or None, y_stride, codes or None, codes_stride,
+                                   scales or None, _stream(stream)))
+
+
+def w8_bytes(outputs: int, inputs: int) -> int:
+    """Device bytes of a packed matrix."""
+    out = np.zeros(1, dtype=np.int64)
+    _check(lib().slora_w8_bytes(outputs, inputs, _ptr(out)))
+    return int(out[0])
+
+
+def w8_pack(outputs: int, inputs: int, dtype: int, codes: int, scales: int, packed: int, stream=None) -> C.c_void_p:
+    """Device addresses; `packed` is borrowed until w8_destroy."""
+    h = C.c_void_p()
+    _check(lib().slora_w8_pack(C.byref(h), outputs, inputs, dtype, codes or None, scales or None, packed or None, _stream(stream)))
+    return h
+
+
+def w8_destroy(w) -> None:
+    _check(lib().slora_w8_destroy(w))
+
+
+def _w8_arrays(handles, xs, x_strides, x_scales, ys, y_strides):
+    n = len(handles)
+    if not n == len(xs) == len(x_strides) == len(x_scales) == len(ys) == len(y_strides):
+        raise ValueError("as many xs, x_strides, x_scales, ys and y_strides as matrices")
+    return _handle_array(handles), _ptr_array(xs), (C.c_int64 * n)(*x_strides), _ptr_array(x_scales), _ptr_array(ys), (C.c_int64 * n)(*y_strides)
+
+
+def w8_matmul(handles, xs: Sequence[int], x_strides: Sequence[int], x_scales: Sequence[int], T: int, ys: Sequence[int], y_strides: Sequence[int],
+              stream=None) -> None:
+    """ys[k] = xs[k] W_k in fp32; x_strides in bytes, y_strides in elements."""
+    h, x, xst, sc, y, yst = _w8_arrays(handles, xs, x_strides, x_scales, ys, y_strides)
+    _check(lib().slora_w8_matmul(len(handles), h, x, xst, sc, T, y, yst, _stream(stream)))
+
+
+def w8_matmul_y16(handles, xs: Sequence[int], x_strides: Sequence[int], x_scales: Sequence[int], T: int, ys: Sequence[int], y_strides: Sequence[int],
+                  stream=None) -> None:
+    """... in the matrices' 16-bit type."""
+    h, x, xst, sc, y, yst = _w8_arrays(handles, xs, x_strides, x_scales, ys, y_strides)
+    _check(lib().slora_w8_matmul_y16(len(handles), h, x, xst, sc, T, y, yst, _stream(stream)))
