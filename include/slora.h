@@ -515,8 +515,8 @@ int32_t slora_w4_matmul_y16(int32_t n, const slora_w4 *const *w, const void *con
  * 8-bit x with 8-bit weights - the base model's xW (Fig. 1) of prompts and of decode batches alike.
  *
  * A row v in 8 bits is its codes and one fp32 scale: with a = max(max |v|, 2^-100),
- *   scale = a / 127,  code = v * (127 / a) rounded to nearest, ties to even (-127 .. 127);  v is about code * scale.
- * Quotients and product are fp32.  A row that holds an infinity or a NaN has codes 0 and a NaN for its scale, so that
+ *   scale = a / 127,  code = v * (1 / a * 127) rounded to nearest, ties to even (-127 .. 127);  v is about code * scale.
+ * Quotients and products are fp32, each rounded.  A row that holds an infinity or a NaN has codes 0 and a NaN for its scale, so that
  * its products are NaN.
  * ------------------------------------------------------------------------------------------- */
 typedef struct slora_norm slora_norm;

@@ -274,7 +274,7 @@ __device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut
 {
     const int top = largest(r, v, team);
     const bool spoiled = top >= 0x7f800000;
-    const float a = fmaxf(__uint_as_float((uint32_t)top), kW8Least), inverse = spoiled ? 0.0f : 127.0f / a;
+    const float a = fmaxf(__uint_as_float((uint32_t)top), kW8Least), inverse = spoiled ? 0.0f : 1.0f / a * 127.0f;
     int8_t *to = out.codes + t * out.codes_stride;
 #pragma unroll
     for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {

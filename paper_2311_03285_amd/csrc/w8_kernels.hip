@@ -13,6 +13,8 @@ namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------
 // packing
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(256) void w8_pack_kernel(const int8_t *__restrict__
 // ---------------------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------------------
-// Matrix instructions 16 x 16 x 64 and 32 x 32 x 32 on 8-bit integers: tokens are rows, outputs columns.  A lane supplies 16 bytes of one row or
+// Matrix instructions 16 x 16 x 64 and 32 x 32 x 32 on 8-bit integers.  A lane supplies 16 bytes of one row or
 // column; which inputs they are does not matter as long as it is the same ones for x and for the weights.
 __device__ __forceinline__ i32x4 mfma16(const i32x4 &a, const i32x4 &b, const i32x4 &c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ i32x16 mfma32(const i32x4 &a, const i32x4 &b, const i32x16 &c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
@@ -56,10 +58,10 @@ __device__ __forceinline__ i32x4 load16b(const int8_t *p) { return *reinterpret_
 
 // Y: 0 fp32, else 1 + the 16-bit type.  The sum, exact so far, is rounded to fp32 and multiplied by both scales there; the product of the scales
 // alone could leave the range that the three have.
+__device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale) { return (float)sum * x_scale * w_scale; }
 template <int Y>
-__device__ __forceinline__ void store_y(void *y, int64_t at, int sum, float x_scale, float w_scale)
+__device__ __forceinline__ void store_y(void *y, int64_t at, float v)
 {
-    const float v = (float)sum * x_scale * w_scale;
     if constexpr (Y == 0)
         static_cast<float *>(y)[at] = v;
     else
@@ -150,31 +152,53 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
         int total = 0;
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k) total += part[k][r / 16 * NT + t / 16][t % 4][t % 16 / 4 * 16 + r % 16];
-        store_y<Y>(m.y, (int64_t)(t0 + t) * m.y_stride + o, total, m.x_scales[t0 + t], m.scales[o]);
+        store_y<Y>(m.y, (int64_t)(t0 + t) * m.y_stride + o, scaled(total, m.x_scales[t0 + t], m.scales[o]));
     }
 }
 
-// Many tokens: a workgroup of four wavefronts, WM x WN of them, takes WM * MT * 32 tokens and WN * NT * 32 outputs, in stages of 128 inputs that go through LDS: two
+// Many tokens: a workgroup of four wavefronts, two by two, takes 2 * MO * 32 outputs and 2 * MT * 32 tokens, in stages of 128 inputs that go through LDS: two
 // buffers, one that is read while the next stage is written to the other, whose bytes have come from memory a stage before.
 // LDS holds units of 16 bytes, [16 rows][chunk of 64][piece of 16][row]: an operand's read is 16 lanes of neighbouring units.  Weights lie so in memory.
 // Rows of x come in eights of pieces (128 bytes); a row's place among 16 is permuted by the piece's number, so that the lanes that write
 // two rows' pieces are in different banks.
+// Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
+// to y in rows.
 constexpr int kTileThreads = 256, kStageBytes = 2 * kW8Chunk;
 
-template <int WM, int WN, int MT, int NT, int Y>
-__global__ __launch_bounds__(kTileThreads, MT * NT > 4 ? 1 : 2) void w8_tile_kernel(W8Args a)
+// what goes beside `mfma` products: reads from LDS, writes to it, loads from memory, each spread evenly
+template <int MFMA, int READS, int WRITES, int LOADS>
+__device__ __forceinline__ void spread()
 {
-    constexpr int BM = WM * MT * 32, BN = WN * NT * 32, kUnits = 8; // units of a row and stage
-    constexpr int kPutsX = BM * kUnits / kTileThreads, kPutsW = BN * kUnits / kTileThreads;
-    extern __shared__ i32x4 lds[]; // [2][BM * kUnits], [2][BN * kUnits]
-    i32x4 *const lds_x = lds, *const lds_w = lds + 2 * BM * kUnits;
+    constexpr int kSlots = MFMA / 2;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, (READS + kSlots - 1) / kSlots, 0);
+        if constexpr (WRITES > 0) __builtin_amdgcn_sched_group_barrier(0x200, (WRITES + kSlots - 1) / kSlots, 0);
+        if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + kSlots - 1) / kSlots, 0);
+    }
+}
+
+template <int MO, int MT>
+constexpr int tile_lds(int y_bytes) // stages, or the outputs of 32 tokens of each wavefront
+{
+    return std::max(2 * (2 * MO * 32 + 2 * MT * 32) * kStageBytes, 4 * 32 * (MO * 32 * y_bytes + 16));
+}
+
+template <int MO, int MT, int Y>
+__global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_kernel(W8Args a)
+{
+    constexpr int BO = 2 * MO * 32, BT = 2 * MT * 32, kUnits = 8; // units of a row and stage
+    constexpr int kPutsX = BT * kUnits / kTileThreads, kPutsW = BO * kUnits / kTileThreads;
+    extern __shared__ i32x4 lds[]; // [2][BT * kUnits], [2][BO * kUnits]
+    i32x4 *const lds_x = lds, *const lds_w = lds + 2 * BT * kUnits;
     const int k = matrix_of(a, blockIdx.x);
     const W8Matrix &m = a.m[k];
     const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 32, h = lane / 32;
-    const int wm = wave / WN, wn = wave % WN;
+    const int wt = wave / 2, wo = wave % 2;
 
-    const int tiles_o = (m.outputs + BN - 1) / BN, block = (int)blockIdx.x - m.first;
-    const int t0 = block / tiles_o * BM, o0 = block % tiles_o * BN;
+    const int tiles_o = (m.outputs + BO - 1) / BO, block = (int)blockIdx.x - m.first;
+    const int t0 = block / tiles_o * BT, o0 = block % tiles_o * BO;
 
     // this thread's unit of a stage, of rows 32 j + threadIdx / 8
     const int piece = threadIdx.x % 8, row0 = threadIdx.x / 8;
@@ -201,23 +225,26 @@ __global__ __launch_bounds__(kTileThreads, MT * NT > 4 ? 1 : 2) void w8_tile_ker
     };
     auto put = [&](int buffer) {
 #pragma unroll
-        for (int j = 0; j < kPutsX; ++j) lds_x[buffer * BM * kUnits + x_put + j * 256] = xr[j];
+        for (int j = 0; j < kPutsX; ++j) lds_x[buffer * BT * kUnits + x_put + j * 256] = xr[j];
 #pragma unroll
-        for (int j = 0; j < kPutsW; ++j) lds_w[buffer * BN * kUnits + threadIdx.x + j * 256] = wr[j];
+        for (int j = 0; j < kPutsW; ++j) lds_w[buffer * BO * kUnits + threadIdx.x + j * 256] = wr[j];
     };
     // units of step ks (32 inputs) of row n: piece 2 ks + h
-    auto read = [&](int buffer, int ks, i32x4 (&x)[MT], i32x4 (&w)[NT]) {
-        const int p = 2 * ks + h, at = p / 4 * 64 + p % 4 * 16;
+    const i32x4 *take_x[4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x[i] = lds_x[buffer * BM * kUnits + ((wm * MT + i) * 2 + n / 16) * 128 + at + ((n % 16) ^ (2 * p))];
+    for (int ks = 0; ks < 4; ++ks) take_x[ks] = lds_x + (wt * MT * 2 + n / 16) * 128 + ks / 2 * 64 + (2 * ks + h) % 4 * 16 + ((n % 16) ^ (2 * (2 * ks + h)));
+    const i32x4 *const take_w = lds_w + (wo * MO * 2 + n / 16) * 128 + h * 16 + n % 16;
+    auto read = [&](int buffer, int ks, i32x4 (&x)[MT], i32x4 (&w)[MO]) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) w[i] = lds_w[buffer * BN * kUnits + ((wn * NT + i) * 2 + n / 16) * 128 + at + n % 16];
+        for (int i = 0; i < MT; ++i) x[i] = take_x[ks][buffer * BT * kUnits + i * 256];
+#pragma unroll
+        for (int i = 0; i < MO; ++i) w[i] = take_w[buffer * BO * kUnits + i * 256 + ks * 32];
     };
-    i32x16 sum[MT][NT];
+    i32x16 sum[MO][MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < MO; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < MT; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[i][j][e] = 0;
 
@@ -225,10 +252,11 @@ __global__ __launch_bounds__(kTileThreads, MT * NT > 4 ? 1 : 2) void w8_tile_ker
     put(0);
     fetch(min(1, stages - 1));
     lds_barrier();
-    i32x4 xf[2][MT], wf[2][NT];
+    i32x4 xf[2][MT], wf[2][MO];
     read(0, 0, xf[0], wf[0]);
     for (int s = 0; s < stages; ++s) {
         const int buffer = s % 2;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             if (ks < 3) {
@@ -237,29 +265,83 @@ __global__ __launch_bounds__(kTileThreads, MT * NT > 4 ? 1 : 2) void w8_tile_ker
                 lds_barrier(); // the next stage is in the other buffer; nobody reads this one any more
                 read(buffer ^ 1, 0, xf[0], wf[0]);
             }
+            if (ks == 0) put(buffer ^ 1); // (behind the last stage: the last once more, which nobody multiplies)
+            if (ks == 1) fetch(min(s + 2, stages - 1));
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < MO; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) sum[i][j] = mfma32(xf[ks % 2][i], wf[ks % 2][j], sum[i][j]);
-            if (ks == 0) {
-                put(buffer ^ 1); // (behind the last stage: the last once more, which nobody multiplies)
-                fetch(min(s + 2, stages - 1));
-            }
+                for (int j = 0; j < MT; ++j) sum[i][j] = mfma32(wf[ks % 2][i], xf[ks % 2][j], sum[i][j]);
+            if (ks == 0)
+                spread<MO * MT, MO + MT, kPutsX + kPutsW, 0>();
+            else if (ks == 1)
+                spread<MO * MT, MO + MT, 0, kPutsX + kPutsW>();
+            else
+                spread<MO * MT, MO + MT, 0, 0>();
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
-    // rows 8 b + 4 h + i of column n are register 4 b + i
+    lds_barrier();
+    // Rows 8 b + 4 h + i of column n are register 4 b + i.  A wavefront's outputs of 32 tokens go through LDS, a token's 16 bytes apart from the next one's end.
+    typedef typename std::conditional<Y == 0, float, uint16_t>::type Out;
+    constexpr int kRow = MO * 32 * (int)sizeof(Out), kPitch = kRow + 16, kLanes = kRow / 16, kEach = 16 / (int)sizeof(Out);
+    char *const stage = reinterpret_cast<char *>(lds) + wave * 32 * kPitch;
+    const int ow = o0 + wo * MO * 32;
+    f32x4 w_scale[MO][4];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int o = o0 + (wn * NT + j) * 32 + n;
-        if (o >= m.outputs) continue;
-        const float w_scale = m.scales[o];
+    for (int i = 0; i < MO; ++i)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int b = 0; b < 4; ++b) w_scale[i][b] = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
+    const bool aligned = m.y_stride % kEach == 0;
+    Out *const y = static_cast<Out *>(m.y);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int t = t0 + (wm * MT + i) * 32 + e / 4 * 8 + 4 * h + e % 4;
-                if (t < a.T) store_y<Y>(m.y, (int64_t)t * m.y_stride + o, sum[i][j][e], m.x_scales[t], w_scale);
+    for (int j = 0; j < MT; ++j) {
+        const int tw = t0 + (wt * MT + j) * 32;
+        const float x_scale = m.x_scales[min(tw + n, a.T - 1)];
+#pragma unroll
+        for (int i = 0; i < MO; ++i)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = scaled(sum[i][j][4 * b + e], x_scale, w_scale[i][b][e]);
+                char *const to = stage + n * kPitch + (i * 32 + 8 * b + 4 * h) * sizeof(Out);
+                if constexpr (Y == 0)
+                    *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
+                else
+                    *reinterpret_cast<u32x2 *>(to) = u32x2{(uint32_t)narrow<Y - 1>(v[0]) | (uint32_t)narrow<Y - 1>(v[1]) << 16,
+                                                           (uint32_t)narrow<Y - 1>(v[2]) | (uint32_t)narrow<Y - 1>(v[3]) << 16};
             }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+        if (aligned) {
+#pragma unroll
+            for (int r = 0; r < 32; r += kWave / kLanes) {
+                const int row = r + lane / kLanes, o = ow + lane % kLanes * kEach;
+                const i32x4 v = *reinterpret_cast<const i32x4 *>(stage + row * kPitch + lane % kLanes * 16);
+                if (tw + row >= a.T) continue;
+                Out *const to = y + (int64_t)(tw + row) * m.y_stride + o;
+                if (o + kEach <= m.outputs) {
+                    *reinterpret_cast<i32x4 *>(to) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e)
+                        if (o + e < m.outputs) to[e] = __builtin_bit_cast(Out, (typename std::conditional<Y == 0, int, uint16_t>::type)((uint32_t)v[e * (int)sizeof(Out) / 4] >> (Y == 0 ? 0 : e % 2 * 16)));
+                }
+            }
+        } else {
+            for (int r = 0; r < 32; ++r) {
+                if (tw + r >= a.T) break;
+#pragma unroll
+                for (int e = 0; e < MO * 32; e += kWave) {
+                    const int o = ow + e + lane;
+                    if (o < m.outputs) y[(int64_t)(tw + r) * m.y_stride + o] = *reinterpret_cast<const Out *>(stage + r * kPitch + (e + lane) * sizeof(Out));
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
     }
 }
 
@@ -285,17 +367,17 @@ int32_t launch_few(W8Args &a, void *stream)
     return check_launch("w8_few");
 }
 
-template <int WM, int WN, int MT, int NT, int Y>
+template <int MO, int MT, int Y>
 int32_t launch_tile(W8Args &a, void *stream)
 {
-    constexpr int BM = WM * MT * 32, BN = WN * NT * 32, kLds = 2 * (BM + BN) * kStageBytes;
-    const int64_t groups = share_out(a, BN, ((int64_t)a.T + BM - 1) / BM);
+    constexpr int BO = 2 * MO * 32, BT = 2 * MT * 32, kLds = tile_lds<MO, MT>(Y == 0 ? 4 : 2);
+    const int64_t groups = share_out(a, BO, ((int64_t)a.T + BT - 1) / BT);
     if (groups * kTileThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", a.T);
     if (kLds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<WM, WN, MT, NT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<MO, MT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
     }
-    hipLaunchKernelGGL((w8_tile_kernel<WM, WN, MT, NT, Y>), dim3((unsigned)groups), dim3(kTileThreads), kLds, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((w8_tile_kernel<MO, MT, Y>), dim3((unsigned)groups), dim3(kTileThreads), kLds, (hipStream_t)stream, a);
     return check_launch("w8_tile");
 }
 
@@ -307,8 +389,8 @@ int32_t by_tokens(W8Args &a, void *stream)
     if (a.T <= 64) return launch_few<1, 4, Y>(a, stream);
     int64_t tiles = 0; // of 256 x 256
     for (int32_t k = 0; k < a.n; ++k) tiles += ((int64_t)a.m[k].outputs + 255) / 256 * (((int64_t)a.T + 255) / 256);
-    if (tiles >= 200) return launch_tile<2, 2, 4, 4, Y>(a, stream);
-    return launch_tile<2, 2, 2, 2, Y>(a, stream);
+    if (tiles >= 200) return launch_tile<4, 4, Y>(a, stream);
+    return launch_tile<2, 2, Y>(a, stream);
 }
 
 } // namespace

@@ -64,7 +64,7 @@ def codes_of(v):
     spoiled = ~np.isfinite(v).all(axis=1)
     with np.errstate(invalid="ignore"):
         a = np.maximum(np.where(spoiled, np.float32(1), np.abs(v).max(axis=1)), np.float32(2.0 ** -100)).astype(np.float32)
-        c = np.rint(v * (np.float32(127) / a)[:, None])
+        c = np.rint(v * (np.float32(1) / a * np.float32(127))[:, None])
     return np.where(spoiled[:, None], 0, c).astype(np.int8), np.where(spoiled, np.float32(np.nan), a / np.float32(127))
 
 
@@ -74,8 +74,8 @@ def codes_within(codes, scales, ref, bound):
     a = np.maximum(np.abs(ref).max(axis=1), 2.0 ** -100)
     ea = bound.max(axis=1)
     assert (np.abs(s - a / 127) <= ea / 127 + 2 * E * a / 127).all()
-    # |v * inverse| <= 127 is rounded three times (quotient, product, scale) before the code is
-    slack = 0.5 * s[:, None] + bound + 127 * 4 * E * s[:, None]
+    # |v * inverse| <= 127 is off by four roundings (quotient, two products, scale) before the code is rounded
+    slack = 0.5 * s[:, None] + bound + 127 * 5 * E * s[:, None]
     assert (np.abs(c * s[:, None] - ref) <= slack).all(), float((np.abs(c * s[:, None] - ref) - slack).max())
     assert np.abs(c).max() <= 127
 
