@@ -160,24 +160,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 // buffers, one that is read while the next stage is written to the other, whose bytes have come from memory a stage before.
 // LDS holds units of 16 bytes, [16 rows][chunk of 64][piece of 16][row]: an operand's read is 16 lanes of neighbouring units.  Weights lie so in memory.
 // Rows of x come in eights of pieces (128 bytes); a row's place among 16 is permuted by the piece's number, so that the lanes that write
-// two rows' pieces are in different banks.
+// eights or sixteens of pieces are in different banks.
 // Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
 // to y in rows.
 constexpr int kTileThreads = 256, kStageBytes = 2 * kW8Chunk;
-
-// what goes beside `mfma` products: reads from LDS, writes to it, loads from memory, each spread evenly
-template <int MFMA, int READS, int WRITES, int LOADS>
-__device__ __forceinline__ void spread()
-{
-    constexpr int kSlots = MFMA / 2;
-#pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-        if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, (READS + kSlots - 1) / kSlots, 0);
-        if constexpr (WRITES > 0) __builtin_amdgcn_sched_group_barrier(0x200, (WRITES + kSlots - 1) / kSlots, 0);
-        if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + kSlots - 1) / kSlots, 0);
-    }
-}
+constexpr int kRaw = 0x00027000; // a buffer of 32-bit words, without a format
 
 template <int MO, int MT>
 constexpr int tile_lds(int y_bytes) // stages, or the outputs of 32 tokens of each wavefront
@@ -189,7 +176,8 @@ template <int MO, int MT, int Y>
 __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_kernel(W8Args a)
 {
     constexpr int BO = 2 * MO * 32, BT = 2 * MT * 32, kUnits = 8; // units of a row and stage
-    constexpr int kPutsX = BT * kUnits / kTileThreads, kPutsW = BO * kUnits / kTileThreads;
+    constexpr int kPutsX = BT * kUnits / kTileThreads, kPutsW = BO * kUnits / kTileThreads, kPuts = kPutsX + kPutsW, kQuarter = kPuts / 4;
+    constexpr int kReads = MT + MO, kBeside = kReads + 2 * kQuarter; // of a step
     extern __shared__ i32x4 lds[]; // [2][BT * kUnits], [2][BO * kUnits]
     i32x4 *const lds_x = lds, *const lds_w = lds + 2 * BT * kUnits;
     const int k = matrix_of(a, blockIdx.x);
@@ -200,45 +188,41 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
     const int tiles_o = (m.outputs + BO - 1) / BO, block = (int)blockIdx.x - m.first;
     const int t0 = block / tiles_o * BT, o0 = block % tiles_o * BO;
 
-    // this thread's unit of a stage, of rows 32 j + threadIdx / 8
+    // This thread's units of a stage: of x, number threadIdx % 8 of rows 32 j + threadIdx / 8; of tiles of 16 outputs 2 j + threadIdx / 128.  Where a row or the last
+    // tile ends inside a stage, loads go on into what is behind, whose weights are 0, as far as the rows of the workgroup, or the codes, reach; loads beyond are 0.
+    const int stages = m.chunks / 2, rows = min(BT, a.T - t0), tiles = min(BO / kW8Rows, m.tiles - o0 / kW8Rows);
+    const auto x_rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(m.x + (int64_t)t0 * m.x_stride), 0, (rows - 1) * m.x_stride + m.x_last + 16, kRaw);
+    const auto w_tiles = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(m.codes + (int64_t)(o0 / kW8Rows) * m.chunks * kW8Block), 0, tiles * m.chunks * kW8Block, kRaw);
     const int piece = threadIdx.x % 8, row0 = threadIdx.x / 8;
-    const int8_t *const x_base = m.x + (int64_t)t0 * m.x_stride;
-    int x_at[kPutsX];
+    auto place = [](int p) { return 2 * p ^ p / 4; }; // permutes the rows of a piece
+    const int x_put = (row0 / 16 * 2 + piece / 4) * 64 + piece % 4 * 16 + ((row0 % 16) ^ place(piece)); // row0 + 32 j: 256 j units on
+    int at[kPuts];
 #pragma unroll
-    for (int j = 0; j < kPutsX; ++j) x_at[j] = min(row0 + 32 * j, a.T - 1 - t0) * m.x_stride;
-    const int x_put = (row0 / 16 * 2 + piece / 4) * 64 + piece % 4 * 16 + ((row0 % 16) ^ (2 * piece)); // row0 + 32 j: 256 j units on
-    // ... of tiles of 16 outputs 2 j + threadIdx / 128
-    const int8_t *const w_base = m.codes + (int64_t)(o0 / kW8Rows) * m.chunks * kW8Block;
-    int w_at[kPutsW];
+    for (int j = 0; j < kPutsX; ++j) at[j] = min(row0 + 32 * j, rows - 1) * m.x_stride + piece * 16;
 #pragma unroll
-    for (int j = 0; j < kPutsW; ++j) w_at[j] = min(2 * j + (int)threadIdx.x / 128, m.tiles - 1 - o0 / kW8Rows) * m.chunks * kW8Block + (int)threadIdx.x % 128 * 16;
-
-    i32x4 xr[kPutsX], wr[kPutsW];
-    const int stages = m.chunks / 2, x_last = m.x_last;
-    auto fetch = [&](int s) {
-        const int at = min(s * kStageBytes + piece * 16, x_last); // (inputs behind the last: weights of 0)
-#pragma unroll
-        for (int j = 0; j < kPutsX; ++j) xr[j] = load16b(x_base + (uint32_t)(x_at[j] + at));
-        const int8_t *const from = w_base + (int64_t)s * 2 * kW8Block;
-#pragma unroll
-        for (int j = 0; j < kPutsW; ++j) wr[j] = load16b(from + (uint32_t)w_at[j]);
+    for (int j = 0; j < kPutsW; ++j) at[kPutsX + j] = min(2 * j + (int)threadIdx.x / 128, tiles - 1) * m.chunks * kW8Block + (int)threadIdx.x % 128 * 16;
+    i32x4 raw[kPuts];
+    auto fetch = [&](int j, int s) {
+        raw[j] = j < kPutsX ? __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x_rows, at[j], s * kStageBytes, 0))
+                            : __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j], s * 2 * kW8Block, 0));
     };
-    auto put = [&](int buffer) {
-#pragma unroll
-        for (int j = 0; j < kPutsX; ++j) lds_x[buffer * BT * kUnits + x_put + j * 256] = xr[j];
-#pragma unroll
-        for (int j = 0; j < kPutsW; ++j) lds_w[buffer * BO * kUnits + threadIdx.x + j * 256] = wr[j];
+    auto put = [&](int j, int buffer) {
+        if (j < kPutsX)
+            lds_x[buffer * BT * kUnits + x_put + j * 256] = raw[j];
+        else
+            lds_w[buffer * BO * kUnits + threadIdx.x + (j - kPutsX) * 256] = raw[j];
     };
     // units of step ks (32 inputs) of row n: piece 2 ks + h
     const i32x4 *take_x[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) take_x[ks] = lds_x + (wt * MT * 2 + n / 16) * 128 + ks / 2 * 64 + (2 * ks + h) % 4 * 16 + ((n % 16) ^ (2 * (2 * ks + h)));
+    for (int ks = 0; ks < 4; ++ks) take_x[ks] = lds_x + (wt * MT * 2 + n / 16) * 128 + ks / 2 * 64 + (2 * ks + h) % 4 * 16 + ((n % 16) ^ place(2 * ks + h));
     const i32x4 *const take_w = lds_w + (wo * MO * 2 + n / 16) * 128 + h * 16 + n % 16;
-    auto read = [&](int buffer, int ks, i32x4 (&x)[MT], i32x4 (&w)[MO]) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) x[i] = take_x[ks][buffer * BT * kUnits + i * 256];
-#pragma unroll
-        for (int i = 0; i < MO; ++i) w[i] = take_w[buffer * BO * kUnits + i * 256 + ks * 32];
+    i32x4 xf[2][MT], wf[2][MO];
+    auto read = [&](int i, int buffer, int ks) {
+        if (i < MT)
+            xf[ks % 2][i] = take_x[ks][buffer * BT * kUnits + i * 256];
+        else
+            wf[ks % 2][i - MT] = take_w[buffer * BO * kUnits + (i - MT) * 256 + ks * 32];
     };
     i32x16 sum[MO][MT];
 #pragma unroll
@@ -248,36 +232,46 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[i][j][e] = 0;
 
-    fetch(0);
-    put(0);
-    fetch(min(1, stages - 1));
+    // A quarter of a stage's units is written in each step.  The buffer that step 3 of a stage leaves takes the first quarter of the stage after next there, and the other
+    // ones in the steps after; registers that have been written take the stage after.
+#pragma unroll
+    for (int j = 0; j < kPuts; ++j) fetch(j, 0);
+#pragma unroll
+    for (int j = 0; j < kPuts; ++j) {
+        put(j, 0);
+        fetch(j, min(1, stages - 1));
+    }
+#pragma unroll
+    for (int j = 0; j < kQuarter; ++j) {
+        put(j, 1);
+        fetch(j, min(2, stages - 1));
+    }
     lds_barrier();
-    i32x4 xf[2][MT], wf[2][MO];
-    read(0, 0, xf[0], wf[0]);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) read(i, 0, 0);
     for (int s = 0; s < stages; ++s) {
         const int buffer = s % 2;
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-            if (ks < 3) {
-                read(buffer, ks + 1, xf[(ks + 1) % 2], wf[(ks + 1) % 2]);
-            } else {
-                lds_barrier(); // the next stage is in the other buffer; nobody reads this one any more
-                read(buffer ^ 1, 0, xf[0], wf[0]);
+            if (ks == 3) lds_barrier(); // the next stage is in the other buffer; nobody reads this one any more
+            // (behind the last stage: the last once more, which nobody multiplies)
+            const int to = ks < 3 ? buffer ^ 1 : buffer, quarter = (ks + 1) % 4, next = min(s + (ks < 3 ? 2 : 3), stages - 1);
+#pragma unroll
+            for (int p = 0; p < MO * MT; ++p) {
+                sum[p / MT][p % MT] = mfma32(wf[ks % 2][p / MT], xf[ks % 2][p % MT], sum[p / MT][p % MT]);
+                // beside each product: operands of the next step first, then units to LDS and from memory in turn
+#pragma unroll
+                for (int o = p * kBeside / (MO * MT); o < (p + 1) * kBeside / (MO * MT); ++o) {
+                    const int j = quarter * kQuarter + (o - kReads) / 2;
+                    if (o < kReads)
+                        read(o, ks < 3 ? buffer : buffer ^ 1, (ks + 1) % 4);
+                    else if ((o - kReads) % 2 == 0)
+                        put(j, to);
+                    else
+                        fetch(j, next);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (ks == 0) put(buffer ^ 1); // (behind the last stage: the last once more, which nobody multiplies)
-            if (ks == 1) fetch(min(s + 2, stages - 1));
-#pragma unroll
-            for (int i = 0; i < MO; ++i)
-#pragma unroll
-                for (int j = 0; j < MT; ++j) sum[i][j] = mfma32(wf[ks % 2][i], xf[ks % 2][j], sum[i][j]);
-            if (ks == 0)
-                spread<MO * MT, MO + MT, kPutsX + kPutsW, 0>();
-            else if (ks == 1)
-                spread<MO * MT, MO + MT, 0, kPutsX + kPutsW>();
-            else
-                spread<MO * MT, MO + MT, 0, 0>();
-            __builtin_amdgcn_sched_barrier(0);
         }
     }
     lds_barrier();
@@ -286,11 +280,6 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
     constexpr int kRow = MO * 32 * (int)sizeof(Out), kPitch = kRow + 16, kLanes = kRow / 16, kEach = 16 / (int)sizeof(Out);
     char *const stage = reinterpret_cast<char *>(lds) + wave * 32 * kPitch;
     const int ow = o0 + wo * MO * 32;
-    f32x4 w_scale[MO][4];
-#pragma unroll
-    for (int i = 0; i < MO; ++i)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) w_scale[i][b] = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
     const bool aligned = m.y_stride % kEach == 0;
     Out *const y = static_cast<Out *>(m.y);
 #pragma unroll
@@ -301,9 +290,10 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
         for (int i = 0; i < MO; ++i)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
+                const f32x4 w_scale = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = scaled(sum[i][j][4 * b + e], x_scale, w_scale[i][b][e]);
+                for (int e = 0; e < 4; ++e) v[e] = scaled(sum[i][j][4 * b + e], x_scale, w_scale[e]);
                 char *const to = stage + n * kPitch + (i * 32 + 8 * b + 4 * h) * sizeof(Out);
                 if constexpr (Y == 0)
                     *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
