@@ -18,18 +18,26 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // ---------------------------------------------------------------------------------------
 // a row in registers
 // ---------------------------------------------------------------------------------------
-// A row belongs to `waves` wavefronts and stays in their registers from its one load to its stores.  Its whole pieces of eight
-// elements are dealt out in turn, P to a lane at most; the elements behind the last whole piece (TAIL) are one more piece of the row's last lane, read and
-// written element by element, so that nothing behind the row is touched.
+// A row belongs to `waves` wavefronts and stays in their registers from its one load to its stores.  Its pieces of eight elements are dealt out in
+// turn, P to a lane at most; a last piece that is not whole (TAIL) is read as the 16-byte words that it begins in, and
+// written element by element, so that nothing behind the row is touched.  (Read by elements it cost norms of 777 rows of 5003 elements 3 of 21 us.)
 // Loads are not behind branches: a lane without a piece reads the row's last one once more.
 template <int P, bool TAIL>
 struct Row {
-    static constexpr int kParts = P + (TAIL ? 1 : 0);
     int lane, lanes; // of the row
-    int pieces, rest; // whole pieces, elements behind them
-    __device__ __forceinline__ bool has(int p) const { return p < P ? lane + p * lanes < pieces : lane == lanes - 1; }
-    __device__ __forceinline__ int at(int p) const { return (p < P ? min(lane + p * lanes, max(pieces - 1, 0)) : pieces) * kPiece; }
-    __device__ __forceinline__ bool valid(int p, int i) const { return has(p) && (p < P || i < rest); }
+    int width, pieces;
+    __device__ __forceinline__ int piece(int p) const { return lane + p * lanes; }
+    __device__ __forceinline__ bool has(int p) const { return piece(p) < pieces; }
+    __device__ __forceinline__ bool whole(int p) const { return !TAIL || (piece(p) + 1) * kPiece <= width; } // of one that there is
+    __device__ __forceinline__ bool valid(int p, int i) const { return TAIL ? piece(p) * kPiece + i < width : has(p); }
+    __device__ __forceinline__ int at(int p) const { return min(piece(p), pieces - 1) * kPiece; }
+    __device__ __forceinline__ int count(int wave) const // elements of a wavefront
+    {
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < P; ++p) n += min(max(width - (p * lanes + wave * kWave) * kPiece, 0), kWave * kPiece);
+        return n;
+    }
 };
 
 template <int DT>
@@ -41,44 +49,30 @@ __device__ __forceinline__ void widen8(const u32x4 &raw, float (&v)[kPiece])
 
 // a 16-bit vector's pieces as they are
 template <int P, bool TAIL>
-__device__ __forceinline__ void load16(const Row<P, TAIL> &r, const uint16_t *from, u32x4 (&raw)[Row<P, TAIL>::kParts])
+__device__ __forceinline__ void load16(const Row<P, TAIL> &r, const uint16_t *from, u32x4 (&raw)[P])
 {
-    if (!TAIL || r.pieces > 0) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) raw[p] = *reinterpret_cast<const u32x4 *>(from + r.at(p));
-    }
-    if constexpr (TAIL) {
-        uint16_t e[kPiece];
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) e[i] = from[r.at(P) + min(i, r.rest - 1)];
-#pragma unroll
-        for (int i = 0; i < kPiece / 2; ++i) raw[P][i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
-    }
+    for (int p = 0; p < P; ++p) raw[p] = *reinterpret_cast<const u32x4 *>(from + r.at(p));
 }
 template <int P, bool TAIL>
-__device__ __forceinline__ void load32(const Row<P, TAIL> &r, const float *from, f32x4 (&raw)[Row<P, TAIL>::kParts][2])
+__device__ __forceinline__ void load32(const Row<P, TAIL> &r, const float *from, f32x4 (&raw)[P][2])
 {
-    if (!TAIL || r.pieces > 0) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) raw[p][i] = *reinterpret_cast<const f32x4 *>(from + r.at(p) + 4 * i);
-    }
-    if constexpr (TAIL) {
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) raw[P][i / 4][i % 4] = from[r.at(P) + min(i, r.rest - 1)];
+    for (int p = 0; p < P; ++p) {
+        raw[p][0] = *reinterpret_cast<const f32x4 *>(from + r.at(p));
+        raw[p][1] = *reinterpret_cast<const f32x4 *>(from + (TAIL ? min(r.at(p) + 4, (r.width - 1) / 4 * 4) : r.at(p) + 4));
     }
 }
 template <int DT, int P, bool TAIL>
-__device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, const float (&v)[Row<P, TAIL>::kParts][kPiece])
+__device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, const float (&v)[P][kPiece])
 {
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+    for (int p = 0; p < P; ++p) {
         if (!r.has(p)) continue;
         uint16_t e[kPiece];
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) e[i] = narrow<DT>(v[p][i]);
-        if (p < P) {
+        if (r.whole(p)) {
             u32x4 u;
 #pragma unroll
             for (int i = 0; i < kPiece / 2; ++i) u[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
@@ -86,23 +80,23 @@ __device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, con
         } else {
 #pragma unroll
             for (int i = 0; i < kPiece - 1; ++i)
-                if (i < r.rest) to[r.at(p) + i] = e[i];
+                if (r.valid(p, i)) to[r.at(p) + i] = e[i];
         }
     }
 }
 template <int P, bool TAIL>
-__device__ __forceinline__ void store32(const Row<P, TAIL> &r, float *to, const float (&v)[Row<P, TAIL>::kParts][kPiece])
+__device__ __forceinline__ void store32(const Row<P, TAIL> &r, float *to, const float (&v)[P][kPiece])
 {
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+    for (int p = 0; p < P; ++p) {
         if (!r.has(p)) continue;
-        if (p < P) {
+        if (r.whole(p)) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4 *>(to + r.at(p) + 4 * i) = f32x4{v[p][4 * i], v[p][4 * i + 1], v[p][4 * i + 2], v[p][4 * i + 3]};
         } else {
 #pragma unroll
             for (int i = 0; i < kPiece - 1; ++i)
-                if (i < r.rest) to[r.at(p) + i] = v[p][i];
+                if (r.valid(p, i)) to[r.at(p) + i] = v[p][i];
         }
     }
 }
@@ -140,15 +134,21 @@ __device__ __forceinline__ int wave_max(int v)
 struct Team {
     uint32_t (*slots)[kRowThreads / kWave];
     int waves, wave, used = 0;
+    // every wavefront's v, behind the next barrier
+    __device__ __forceinline__ const float *share(float v)
+    {
+        float *s = reinterpret_cast<float *>(slots[used++]);
+        if (threadIdx.x % kWave == 0) s[wave] = v;
+        return s;
+    }
     __device__ __forceinline__ float sum(float v)
     {
         v = wave_sum(v);
         if (waves == 1) return v;
-        uint32_t *s = slots[used++];
-        if (threadIdx.x % kWave == 0) s[wave] = __float_as_uint(v);
+        const float *const s = share(v);
         __syncthreads();
         v = 0.0f;
-        for (int w = 0; w < waves; ++w) v += __uint_as_float(s[w]);
+        for (int w = 0; w < waves; ++w) v += s[w];
         return v;
     }
     __device__ __forceinline__ int max_of(int v)
@@ -169,11 +169,11 @@ constexpr int kReductions = 11; // most of a row: two norms of five (mean, sprea
 __device__ __forceinline__ int magnitude(float v) { return (int)(__float_as_uint(v) & 0x7fffffffu); }
 
 template <int P, bool TAIL>
-__device__ __forceinline__ int largest(const Row<P, TAIL> &r, const float (&v)[Row<P, TAIL>::kParts][kPiece], Team &team)
+__device__ __forceinline__ int largest(const Row<P, TAIL> &r, const float (&v)[P][kPiece], Team &team)
 {
     int top = 0;
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+    for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) top = max(top, r.valid(p, i) ? magnitude(v[p][i]) : 0);
     return team.max_of(top);
@@ -185,27 +185,43 @@ __device__ __forceinline__ int largest(const Row<P, TAIL> &r, const float (&v)[R
 struct Spread {
     float mean, square; // square: mean square of v - mean
 };
+// Layer norms: each wavefront's mean and its sum of squares about that, put together with one barrier: the squares about the row's mean are
+// those plus count * (difference of means)^2.  All terms are positive; nothing cancels.
 template <int P, bool TAIL>
-__device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (&v)[Row<P, TAIL>::kParts][kPiece], bool layer, int width, Team &team)
+__device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (&v)[P][kPiece], bool layer, int width, Team &team)
 {
     Spread s{0.0f, 0.0f};
     if (layer) {
         float sum = 0.0f;
 #pragma unroll
-        for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) sum += r.valid(p, i) ? v[p][i] : 0.0f;
-        s.mean = team.sum(sum) / (float)width;
+        s.mean = wave_sum(sum) / (float)max(r.count(team.waves == 1 ? 0 : team.wave), 1);
     }
     float sum = 0.0f;
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+    for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) {
             const float d = r.valid(p, i) ? v[p][i] - s.mean : 0.0f;
             sum = __builtin_fmaf(d, d, sum);
         }
-    s.square = team.sum(sum) / (float)width;
+    if (layer && team.waves > 1) {
+        const float *const square = team.share(wave_sum(sum)), *const mean = team.share(s.mean);
+        __syncthreads();
+        float total = 0.0f;
+        for (int w = 0; w < team.waves; ++w) total = __builtin_fmaf(mean[w], (float)r.count(w), total);
+        s.mean = total / (float)width;
+        total = 0.0f;
+        for (int w = 0; w < team.waves; ++w) {
+            const float d = mean[w] - s.mean;
+            total += __builtin_fmaf(d * d, (float)r.count(w), square[w]);
+        }
+        s.square = total / (float)width;
+    } else {
+        s.square = team.sum(sum) / (float)width;
+    }
     return s;
 }
 
@@ -213,7 +229,7 @@ __device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (
 // Squares that leave fp32's range (bfloat16 and fp32 rows can) are taken again of v times a power of two, which is
 // exact; eps, which is 0 or at least 2^-60, is then 0 or negligible or scaled along.  All lanes of the row go the same way.
 template <int P, bool TAIL>
-__device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[Row<P, TAIL>::kParts][kPiece], bool layer, int width, float eps, Team &team)
+__device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[P][kPiece], bool layer, int width, float eps, Team &team)
 {
     Spread s = spread_of(r, v, layer, width, team);
     float q = s.square + eps;
@@ -224,7 +240,7 @@ __device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[Row<
             const int up = 127 - max(top >> 23, 1);
             const float a = __uint_as_float((uint32_t)(127 + up / 2) << 23), b = __uint_as_float((uint32_t)(127 + (up - up / 2)) << 23);
 #pragma unroll
-            for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+            for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) v[p][i] = v[p][i] * a * b;
             s = spread_of(r, v, layer, width, team);
@@ -233,19 +249,19 @@ __device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[Row<
     }
     const float by = 1.0f / sqrtf(q);
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p)
+    for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) v[p][i] = (v[p][i] - s.mean) * by;
 }
 
 // v = v * weight + bias, where there are any
 template <int DT, int P, bool TAIL>
-__device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[Row<P, TAIL>::kParts][kPiece], const u32x4 (&weight)[Row<P, TAIL>::kParts], const uint16_t *w,
+__device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[P][kPiece], const u32x4 (&weight)[P], const uint16_t *w,
                                        const uint16_t *bias)
 {
     if (w) {
 #pragma unroll
-        for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+        for (int p = 0; p < P; ++p) {
             float e[kPiece];
             widen8<DT>(weight[p], e);
 #pragma unroll
@@ -253,10 +269,10 @@ __device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[Row<P, 
         }
     }
     if (bias) {
-        u32x4 raw[Row<P, TAIL>::kParts];
+        u32x4 raw[P];
         load16(r, bias, raw);
 #pragma unroll
-        for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+        for (int p = 0; p < P; ++p) {
             float e[kPiece];
             widen8<DT>(raw[p], e);
 #pragma unroll
@@ -270,19 +286,19 @@ __device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[Row<P, 
 // ---------------------------------------------------------------------------------------
 // Codes are rounded from fp32 values (not from the 16 bits that x is rounded to: one rounding, not two).
 template <int P, bool TAIL>
-__device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut &out, int64_t t, const float (&v)[Row<P, TAIL>::kParts][kPiece], Team &team)
+__device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut &out, int64_t t, const float (&v)[P][kPiece], Team &team)
 {
     const int top = largest(r, v, team);
     const bool spoiled = top >= 0x7f800000;
     const float a = fmaxf(__uint_as_float((uint32_t)top), kW8Least), inverse = spoiled ? 0.0f : 1.0f / a * 127.0f;
     int8_t *to = out.codes + t * out.codes_stride;
 #pragma unroll
-    for (int p = 0; p < Row<P, TAIL>::kParts; ++p) {
+    for (int p = 0; p < P; ++p) {
         if (!r.has(p)) continue;
         uint32_t c[kPiece];
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) c[i] = spoiled ? 0u : (uint32_t)(int)__builtin_rintf(v[p][i] * inverse) & 0xffu;
-        if (p < P) {
+        if (r.whole(p)) {
             u32x2 u;
 #pragma unroll
             for (int i = 0; i < 2; ++i) u[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | c[4 * i + 3] << 24;
@@ -290,7 +306,7 @@ __device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut
         } else {
 #pragma unroll
             for (int i = 0; i < kPiece - 1; ++i)
-                if (i < r.rest) to[r.at(p) + i] = (int8_t)c[i];
+                if (r.valid(p, i)) to[r.at(p) + i] = (int8_t)c[i];
         }
     }
     if (r.lane == 0) out.scales[t] = spoiled ? __uint_as_float(0x7fc00000u) : a / 127.0f;
@@ -304,8 +320,8 @@ __device__ __forceinline__ Row<P, TAIL> row_of(int width, int waves)
     Row<P, TAIL> r;
     r.lanes = waves * kWave;
     r.lane = waves == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
-    r.pieces = width / kPiece;
-    r.rest = width % kPiece;
+    r.width = width;
+    r.pieces = (width + kPiece - 1) / kPiece;
     return r;
 }
 
@@ -316,11 +332,11 @@ __device__ __forceinline__ int64_t row_number(int waves, int wave)
 }
 
 // One row for the workgroup, or (waves == 1) one for each of its wavefronts.
-// Bound: HBM.
+// Bound: HBM where there are rows enough (8192 rows of 8192, a norm behind the block and a gate by channel, 537 MB: 97 us = 5.5 TB/s, a copy reaches 5.05; 2048
+// of 4096 14.9 us = 4.5 TB/s); below, the chain of two loads, two to four reductions and a store (777 rows of 5003 in fp32, gate by token: 20 us = 2.7 TB/s), and the launch (one row 6.5 us).
 template <int DT, bool H32, int P, bool TAIL>
 __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves)
 {
-    constexpr int kParts = Row<P, TAIL>::kParts;
     __shared__ uint32_t slots[kReductions][kRowThreads / kWave];
     const int wave = wave_number();
     const int64_t t = row_number(waves, wave);
@@ -328,13 +344,14 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
     const Row<P, TAIL> r = row_of<P, TAIL>(a.width, waves);
     Team team{slots, waves, wave};
 
-    // With four pieces a lane there are no registers for what is not needed yet: 128 of them, where a workgroup may have 16 wavefronts.
+    // With four pieces a lane nothing is loaded before it is needed: what is under way early takes registers that more wavefronts can use.  us with / without: 2048
+    // rows of 16384 54 / 51, 8192 of 8192 98 / 96, 777 of 5003 20 / 20.
     constexpr bool kAhead = P <= 2;
     auto not_before = [] {
         if constexpr (!kAhead) asm volatile("" ::: "memory");
     };
-    float v[kParts][kPiece];
-    typedef typename std::conditional<H32, f32x4[kParts][2], u32x4[kParts]>::type Raw;
+    float v[P][kPiece];
+    typedef typename std::conditional<H32, f32x4[P][2], u32x4[P]>::type Raw;
     Raw h;
     auto load_h = [&] {
         if constexpr (H32)
@@ -344,7 +361,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
     };
     if constexpr (kAhead) load_h();
     if (a.block) {
-        u32x4 raw[kParts], weight[kParts], gate[kParts];
+        u32x4 raw[P], weight[P], gate[P];
         auto load_weight = [&] {
             if (a.post && a.post_weight) load16(r, a.post_weight, weight);
         };
@@ -355,7 +372,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
         if constexpr (kAhead) load_weight();
         if constexpr (kAhead) load_gate();
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) widen8<DT>(raw[p], v[p]);
+        for (int p = 0; p < P; ++p) widen8<DT>(raw[p], v[p]);
         if (a.post) {
             normalise(r, v, a.layer != 0, a.width, a.eps, team);
             not_before();
@@ -366,7 +383,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
         if constexpr (!kAhead) load_gate();
         if (a.gate) {
 #pragma unroll
-            for (int p = 0; p < kParts; ++p) {
+            for (int p = 0; p < P; ++p) {
                 float e[kPiece];
                 widen8<DT>(gate[p], e);
 #pragma unroll
@@ -377,7 +394,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
     not_before();
     if constexpr (!kAhead) load_h();
 #pragma unroll
-    for (int p = 0; p < kParts; ++p) {
+    for (int p = 0; p < P; ++p) {
         float e[kPiece];
         if constexpr (H32) {
 #pragma unroll
@@ -395,7 +412,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
             store16<DT>(r, static_cast<uint16_t *>(a.h_out) + t * a.h_out_stride, v);
     }
     if (!a.out.x && !a.out.codes) return;
-    u32x4 weight[kParts];
+    u32x4 weight[P];
     auto load_weight = [&] {
         if (a.pre_weight) load16(r, a.pre_weight, weight);
     };
@@ -408,23 +425,24 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
     if (a.out.codes) store_codes(r, a.out, t, v, team);
 }
 
-// ... as above
+// ... as above.  exp and 1 / (1 + exp) are the hardware's, good to a step each (with expf and a division, which are longer than the row takes to load, 3001
+// rows of 13007 took 62 us); where exp(-u) leaves fp32's range (u < -88) or 1 + exp(-u) passes 2^126, the product is 0.
+// Bound: HBM (3001 gated rows of 13007, 234 MB: 44 us = 5.3 TB/s; 4096 rows of 5120 to 8 bits, 63 MB: 15 us = 4.2 TB/s).
 template <int DT, int P, bool TAIL>
 __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, int waves)
 {
-    constexpr int kParts = Row<P, TAIL>::kParts;
     __shared__ uint32_t slots[1][kRowThreads / kWave];
     const int wave = wave_number();
     const int64_t t = row_number(waves, wave);
     if (t >= a.T) return;
     const Row<P, TAIL> r = row_of<P, TAIL>(a.width, waves);
     Team team{slots, waves, wave};
-    u32x4 raw[kParts], gate[kParts];
+    u32x4 raw[P], gate[P];
     load16(r, a.x + t * a.x_stride, raw);
     if (a.gate) load16(r, a.gate + t * a.gate_stride, gate);
-    float v[kParts][kPiece];
+    float v[P][kPiece];
 #pragma unroll
-    for (int p = 0; p < kParts; ++p) {
+    for (int p = 0; p < P; ++p) {
         widen8<DT>(raw[p], v[p]);
         if (a.gate) {
             float g[kPiece];
@@ -433,7 +451,7 @@ __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, i
             for (int i = 0; i < kPiece; ++i) {
                 // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
                 const float u = a.act == SLORA_ACT_SILU ? g[i] : 1.5957691216057308f * __builtin_fmaf(0.044715f * g[i] * g[i], g[i], g[i]);
-                v[p][i] *= g[i] / (1.0f + expf(-u));
+                v[p][i] *= g[i] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.44269504088896340736f));
             }
         }
     }
@@ -441,15 +459,20 @@ __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, i
     if (a.out.codes) store_codes(r, a.out, t, v, team);
 }
 
-// f(pieces of a lane, wavefronts of a row)
+// f(pieces of a lane, wavefronts of a row), by the width alone, so that a row's result does not depend on the others.
+// Norms of rows of more than 2048 elements hold four pieces a lane, so that fewer wavefronts wait for each other.  us with two / four: 2048 rows of 4096 17.2 / 14.9, of
+// 16384 64 / 51, 8192 of 8192 99 / 97, 777 of 5003 21.7 / 20.0, 8192 of 4096 without a norm behind the block 48 / 49; up to 1024 elements one
+// wavefront has the row: 16384 of 1024 25 with two, 27 with four pieces, of 128 7.8 with one, 14 with four.
+// Rows in 8 bits hold two up to 16384: 4096 of 5120 15 / 15, gated 3001 of 13007 44 / 47.
 template <int MOST, typename F>
 int32_t by_width(int width, F f)
 {
-    const int pieces = std::max(width / kPiece, 1);
+    const int pieces = (width + kPiece - 1) / kPiece;
     auto waves = [&](int p) { return (pieces + p * kWave - 1) / (p * kWave); };
     if (waves(1) <= 1) return f(std::integral_constant<int, 1>{}, 1);
-    if (waves(2) <= 16) return f(std::integral_constant<int, 2>{}, waves(2));
-    if constexpr (MOST == 8) {
+    if (waves(4) <= 1) return f(std::integral_constant<int, 2>{}, waves(2));
+    if constexpr (MOST == 8) { // rows in 8 bits
+        if (waves(2) <= 16) return f(std::integral_constant<int, 2>{}, waves(2));
         if (waves(4) > 16) return f(std::integral_constant<int, 8>{}, waves(8));
     }
     return f(std::integral_constant<int, 4>{}, waves(4));

@@ -156,61 +156,84 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
     }
 }
 
-// Many tokens: a workgroup of four wavefronts, two by two, takes 2 * MO * 32 outputs and 2 * MT * 32 tokens, in stages of 128 inputs that go through LDS: two
+// Many tokens: a workgroup takes WO * MO * 32 outputs and WT * MT * 32 tokens, WO x WT wavefronts of them, in stages of 128 inputs that go through LDS: two
 // buffers, one that is read while the next stage is written to the other, whose bytes have come from memory a stage before.
+// Where that gives few workgroups, TEAMS of such wavefronts take stages in turn, each through buffers of its own, and are added up at the end.
 // LDS holds units of 16 bytes, [16 rows][chunk of 64][piece of 16][row]: an operand's read is 16 lanes of neighbouring units.  Weights lie so in memory.
 // Rows of x come in eights of pieces (128 bytes); a row's place among 16 is permuted by the piece's number, so that the lanes that write
 // eights or sixteens of pieces are in different banks.
 // Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
 // to y in rows.
-constexpr int kTileThreads = 256, kStageBytes = 2 * kW8Chunk;
+constexpr int kStageBytes = 2 * kW8Chunk;
 constexpr int kRaw = 0x00027000; // a buffer of 32-bit words, without a format
+constexpr int kNowhere = 1 << 30; // an offset behind every buffer's end: loads are 0
 
-template <int MO, int MT>
-constexpr int tile_lds(int y_bytes) // stages, or the outputs of 32 tokens of each wavefront
-{
-    return std::max(2 * (2 * MO * 32 + 2 * MT * 32) * kStageBytes, 4 * 32 * (MO * 32 * y_bytes + 16));
-}
+template <int TEAMS, int WO, int WT, int MO, int MT>
+struct Tile {
+    static constexpr int kTeam = WO * WT * kWave, kThreads = TEAMS * kTeam; // threads
+    static constexpr int BO = WO * MO * 32, BT = WT * MT * 32, kUnits = 8;  // units of a row and stage
+    static constexpr int kStages = 2 * (BO + BT) * kUnits;                  // of a team
+    static constexpr int kWaves = kThreads / kWave;
+    static constexpr int lds(int y_bytes) // stages, or all teams' sums but one's, or the outputs of 32 tokens of each wavefront
+    {
+        const int pitch = MO * 32 * y_bytes + 16;
+        return std::max({TEAMS * kStages * 16, (TEAMS - 1) * kTeam * MO * MT * 64, WO * WT * 32 * pitch});
+    }
+};
+// wavefronts of a SIMD: with 144 sums a lane and more there is one
+constexpr int tile_occupancy(int blocks) { return blocks >= 8 ? 1 : 2; }
 
-template <int MO, int MT, int Y>
-__global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_kernel(W8Args a)
+template <int TEAMS, int WO, int WT, int MO, int MT, int Y>
+__global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void w8_tile_kernel(W8Args a)
 {
-    constexpr int BO = 2 * MO * 32, BT = 2 * MT * 32, kUnits = 8; // units of a row and stage
-    constexpr int kPutsX = BT * kUnits / kTileThreads, kPutsW = BO * kUnits / kTileThreads, kPuts = kPutsX + kPutsW, kQuarter = kPuts / 4;
-    constexpr int kReads = MT + MO, kBeside = kReads + 2 * kQuarter; // of a step
-    extern __shared__ i32x4 lds[]; // [2][BT * kUnits], [2][BO * kUnits]
-    i32x4 *const lds_x = lds, *const lds_w = lds + 2 * BT * kUnits;
+    typedef Tile<TEAMS, WO, WT, MO, MT> Shape;
+    constexpr int BO = Shape::BO, BT = Shape::BT, kUnits = Shape::kUnits, kTeam = Shape::kTeam;
+    constexpr int kPutsX = BT * kUnits / kTeam, kPutsW = BO * kUnits / kTeam, kPuts = kPutsX + kPutsW; // units of a thread and stage
+    constexpr int kReads = MT + MO;
+    extern __shared__ i32x4 lds[]; // [team] {[2][BT * kUnits], [2][BO * kUnits]}
     const int k = matrix_of(a, blockIdx.x);
     const W8Matrix &m = a.m[k];
-    const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 32, h = lane / 32;
-    const int wt = wave / 2, wo = wave % 2;
+    const int wave = wave_number() % (WO * WT), team = wave_number() / (WO * WT), thread = threadIdx.x % kTeam, lane = threadIdx.x % kWave, n = lane % 32, h = lane / 32;
+    const int wt = wave / WO, wo = wave % WO;
+    i32x4 *const lds_x = lds + team * Shape::kStages, *const lds_w = lds_x + 2 * BT * kUnits;
 
+    // (Giving each die a run of neighbouring tiles was no faster: 8192 tokens of 8192 x 8192 464 - 468 us either way, 5376 of 5120 237 / 243.)
     const int tiles_o = (m.outputs + BO - 1) / BO, block = (int)blockIdx.x - m.first;
     const int t0 = block / tiles_o * BT, o0 = block % tiles_o * BO;
 
-    // This thread's units of a stage: of x, number threadIdx % 8 of rows 32 j + threadIdx / 8; of tiles of 16 outputs 2 j + threadIdx / 128.  Where a row or the last
+    // This thread's units of a stage: of x, number thread % 8 of rows thread / 8 and on; of the weights, number thread and on.  Where a row or the last
     // tile ends inside a stage, loads go on into what is behind, whose weights are 0, as far as the rows of the workgroup, or the codes, reach; loads beyond are 0.
     const int stages = m.chunks / 2, rows = min(BT, a.T - t0), tiles = min(BO / kW8Rows, m.tiles - o0 / kW8Rows);
     const auto x_rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(m.x + (int64_t)t0 * m.x_stride), 0, (rows - 1) * m.x_stride + m.x_last + 16, kRaw);
     const auto w_tiles = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(m.codes + (int64_t)(o0 / kW8Rows) * m.chunks * kW8Block), 0, tiles * m.chunks * kW8Block, kRaw);
-    const int piece = threadIdx.x % 8, row0 = threadIdx.x / 8;
+    const int piece = thread % 8, row0 = thread / 8;
     auto place = [](int p) { return 2 * p ^ p / 4; }; // permutes the rows of a piece
-    const int x_put = (row0 / 16 * 2 + piece / 4) * 64 + piece % 4 * 16 + ((row0 % 16) ^ place(piece)); // row0 + 32 j: 256 j units on
+    const auto x_put = [&](int j) { // (constant steps of j where a team has 16 rows of threads or more)
+        const int row = row0 + j * (kTeam / 8);
+        return (row / 16 * 2 + piece / 4) * 64 + piece % 4 * 16 + ((row % 16) ^ place(piece));
+    };
     int at[kPuts];
 #pragma unroll
-    for (int j = 0; j < kPutsX; ++j) at[j] = min(row0 + 32 * j, rows - 1) * m.x_stride + piece * 16;
+    for (int j = 0; j < kPutsX; ++j) at[j] = min(row0 + j * (kTeam / 8), rows - 1) * m.x_stride + piece * 16;
 #pragma unroll
-    for (int j = 0; j < kPutsW; ++j) at[kPutsX + j] = min(2 * j + (int)threadIdx.x / 128, tiles - 1) * m.chunks * kW8Block + (int)threadIdx.x % 128 * 16;
+    for (int j = 0; j < kPutsW; ++j) {
+        const int u = thread + j * kTeam;
+        at[kPutsX + j] = min(u / 128, tiles - 1) * m.chunks * kW8Block + u % 128 * 16;
+    }
     i32x4 raw[kPuts];
-    auto fetch = [&](int j, int s) {
-        raw[j] = j < kPutsX ? __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x_rows, at[j], s * kStageBytes, 0))
-                            : __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j], s * 2 * kW8Block, 0));
+    auto fetch = [&](int j, int s) { // turn s of this team
+
+        const int number = s * TEAMS + team;
+        if (j < kPutsX)
+            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x_rows, at[j] + (number < stages ? number * kStageBytes : kNowhere), 0, 0));
+        else
+            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j] + (number < stages ? number * (2 * kW8Block) : kNowhere), 0, 0));
     };
     auto put = [&](int j, int buffer) {
         if (j < kPutsX)
-            lds_x[buffer * BT * kUnits + x_put + j * 256] = raw[j];
+            lds_x[buffer * BT * kUnits + x_put(j)] = raw[j];
         else
-            lds_w[buffer * BO * kUnits + threadIdx.x + (j - kPutsX) * 256] = raw[j];
+            lds_w[buffer * BO * kUnits + thread + (j - kPutsX) * kTeam] = raw[j];
     };
     // units of step ks (32 inputs) of row n: piece 2 ks + h
     const i32x4 *take_x[4];
@@ -232,49 +255,79 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[i][j][e] = 0;
 
-    // A quarter of a stage's units is written in each step.  The buffer that step 3 of a stage leaves takes the first quarter of the stage after next there, and the other
-    // ones in the steps after; registers that have been written take the stage after.
+    // Operands are read a step ahead, and a quarter of a stage's units is written in each step.  The buffer that step 3 leaves takes the first quarter of the stage after
+    // next there, and the other ones in the steps that follow; registers that have been written take the stage after that.  (Behind the last stage: zeros.)
+    // More of either, operands two steps and units two or three stages ahead, was no faster (512 tokens of 4096 x 4096, cold weights, 22 us each).
+    auto quarter = [](int q) { return q * kPuts / 4; };
+    const int turns = (stages + TEAMS - 1) / TEAMS;
 #pragma unroll
     for (int j = 0; j < kPuts; ++j) fetch(j, 0);
 #pragma unroll
     for (int j = 0; j < kPuts; ++j) {
         put(j, 0);
-        fetch(j, min(1, stages - 1));
+        fetch(j, 1);
     }
 #pragma unroll
-    for (int j = 0; j < kQuarter; ++j) {
+    for (int j = 0; j < quarter(1); ++j) {
         put(j, 1);
-        fetch(j, min(2, stages - 1));
+        fetch(j, 2);
     }
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < kReads; ++i) read(i, 0, 0);
-    for (int s = 0; s < stages; ++s) {
+    for (int s = 0; s < turns; ++s) {
         const int buffer = s % 2;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-            if (ks == 3) lds_barrier(); // the next stage is in the other buffer; nobody reads this one any more
-            // (behind the last stage: the last once more, which nobody multiplies)
-            const int to = ks < 3 ? buffer ^ 1 : buffer, quarter = (ks + 1) % 4, next = min(s + (ks < 3 ? 2 : 3), stages - 1);
+            const bool crosses = ks == 3;
+            if (crosses) lds_barrier(); // the next stage is in the other buffer; nobody reads this one any more
+            const int q = (ks + 1) % 4, beside = kReads + 2 * (quarter(q + 1) - quarter(q));
 #pragma unroll
             for (int p = 0; p < MO * MT; ++p) {
                 sum[p / MT][p % MT] = mfma32(wf[ks % 2][p / MT], xf[ks % 2][p % MT], sum[p / MT][p % MT]);
-                // beside each product: operands of the next step first, then units to LDS and from memory in turn
+                // beside each product: operands first, then units to LDS and from memory in turn
 #pragma unroll
-                for (int o = p * kBeside / (MO * MT); o < (p + 1) * kBeside / (MO * MT); ++o) {
-                    const int j = quarter * kQuarter + (o - kReads) / 2;
+                for (int o = p * beside / (MO * MT); o < (p + 1) * beside / (MO * MT); ++o) {
+                    const int j = quarter(q) + (o - kReads) / 2;
                     if (o < kReads)
-                        read(o, ks < 3 ? buffer : buffer ^ 1, (ks + 1) % 4);
+                        read(o, crosses ? buffer ^ 1 : buffer, q);
                     else if ((o - kReads) % 2 == 0)
-                        put(j, to);
+                        put(j, crosses ? buffer : buffer ^ 1);
                     else
-                        fetch(j, next);
+                        fetch(j, s + (crosses ? 3 : 2));
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    if constexpr (TEAMS > 1) { // the other teams' sums to the first
+        lds_barrier();
+        i32x4 *const merge = lds + (team - 1) * kTeam * MO * MT * 4 + thread;
+        if (team > 0) {
+#pragma unroll
+            for (int i = 0; i < MO * MT; ++i)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const i32x16 &v = sum[i / MT][i % MT];
+                    merge[(i * 4 + b) * kTeam] = i32x4{v[4 * b], v[4 * b + 1], v[4 * b + 2], v[4 * b + 3]};
+                }
+        }
+        lds_barrier();
+        if (team == 0) {
+#pragma unroll
+            for (int k = 1; k < TEAMS; ++k)
+#pragma unroll
+                for (int i = 0; i < MO * MT; ++i)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const i32x4 v = lds[(k - 1) * kTeam * MO * MT * 4 + thread + (i * 4 + b) * kTeam];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[i / MT][i % MT][4 * b + e] += v[e];
+                    }
+        }
+    }
     lds_barrier();
+    if (team > 0) return;
     // Rows 8 b + 4 h + i of column n are register 4 b + i.  A wavefront's outputs of 32 tokens go through LDS, a token's 16 bytes apart from the next one's end.
     typedef typename std::conditional<Y == 0, float, uint16_t>::type Out;
     constexpr int kRow = MO * 32 * (int)sizeof(Out), kPitch = kRow + 16, kLanes = kRow / 16, kEach = 16 / (int)sizeof(Out);
@@ -320,13 +373,10 @@ __global__ __launch_bounds__(kTileThreads, MO * MT > 4 ? 1 : 2) void w8_tile_ker
                 }
             }
         } else {
-            for (int r = 0; r < 32; ++r) {
-                if (tw + r >= a.T) break;
-#pragma unroll
-                for (int e = 0; e < MO * 32; e += kWave) {
-                    const int o = ow + e + lane;
-                    if (o < m.outputs) y[(int64_t)(tw + r) * m.y_stride + o] = *reinterpret_cast<const Out *>(stage + r * kPitch + (e + lane) * sizeof(Out));
-                }
+#pragma unroll 8
+            for (int i = lane; i < 32 * MO * 32; i += kWave) {
+                const int row = i / (MO * 32), e = i % (MO * 32);
+                if (tw + row < a.T && ow + e < m.outputs) y[(int64_t)(tw + row) * m.y_stride + ow + e] = *reinterpret_cast<const Out *>(stage + row * kPitch + e * sizeof(Out));
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
@@ -357,30 +407,76 @@ int32_t launch_few(W8Args &a, void *stream)
     return check_launch("w8_few");
 }
 
-template <int MO, int MT, int Y>
+template <int TEAMS, int WO, int WT, int MO, int MT, int Y>
 int32_t launch_tile(W8Args &a, void *stream)
 {
-    constexpr int BO = 2 * MO * 32, BT = 2 * MT * 32, kLds = tile_lds<MO, MT>(Y == 0 ? 4 : 2);
-    const int64_t groups = share_out(a, BO, ((int64_t)a.T + BT - 1) / BT);
-    if (groups * kTileThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", a.T);
+    typedef Tile<TEAMS, WO, WT, MO, MT> Shape;
+    constexpr int kLds = Shape::lds(Y == 0 ? 4 : 2);
+    static_assert(kLds <= 160 * 1024, "LDS");
+    const int64_t groups = share_out(a, Shape::BO, ((int64_t)a.T + Shape::BT - 1) / Shape::BT);
+    if (groups * Shape::kThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", a.T);
     if (kLds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<MO, MT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<TEAMS, WO, WT, MO, MT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
     }
-    hipLaunchKernelGGL((w8_tile_kernel<MO, MT, Y>), dim3((unsigned)groups), dim3(kTileThreads), kLds, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((w8_tile_kernel<TEAMS, WO, WT, MO, MT, Y>), dim3((unsigned)groups), dim3(Shape::kThreads), kLds, (hipStream_t)stream, a);
     return check_launch("w8_tile");
 }
 
-template <int Y>
-int32_t by_tokens(W8Args &a, void *stream)
+constexpr int64_t kComputeUnits = 256;
+
+// How many of `each` outputs there are.
+int64_t parts(const W8Args &a, int each)
 {
-    if (a.T <= 16) return launch_few<1, 1, Y>(a, stream);
-    if (a.T <= 32) return launch_few<1, 2, Y>(a, stream);
-    if (a.T <= 64) return launch_few<1, 4, Y>(a, stream);
-    int64_t tiles = 0; // of 256 x 256
-    for (int32_t k = 0; k < a.n; ++k) tiles += ((int64_t)a.m[k].outputs + 255) / 256 * (((int64_t)a.T + 255) / 256);
-    if (tiles >= 200) return launch_tile<4, 4, Y>(a, stream);
-    return launch_tile<2, 2, Y>(a, stream);
+    int64_t n = 0;
+    for (int32_t k = 0; k < a.n; ++k) n += ((int64_t)a.m[k].outputs + each - 1) / each;
+    return n;
+}
+int64_t rounds(int64_t groups) { return (groups + kComputeUnits - 1) / kComputeUnits; }
+
+// Up to 16 tokens: one tile of outputs a workgroup or two, by the bytes that the compute unit with most workgroups reads.  us with one / two: 16 tokens, two of 20480 of
+// 5120 52 / 39, 5120 of 20480 37 / 28, 4096 of 4096 5.8 / 6.7; 8 tokens, three of 4096 of 4096 10.6 / 11.3.
+template <int Y>
+int32_t few(W8Args &a, void *stream)
+{
+    const int64_t tiles = parts(a, kW8Rows);
+    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T)) return launch_few<1, 1, Y>(a, stream);
+    return launch_few<2, 1, Y>(a, stream);
+}
+
+// More tokens: the shape whose workgroups, of which compute units take rounds, are done first, by what a stage of one takes (measured with one and with
+// several rounds, where clocks are lower).  The larger the shape, the less is read for each product; the smaller, the more compute units have one.
+// us: 256 x 256 against the next ones, 8192 tokens of 8192 x 8192 453 / 500 / 519, two of 20480 of 5120, 2048 tokens 387 / 418 / 441; 256 x 192 / 256 x 256, 5120 of
+// 20480, 2048 tokens 197 / 211; 256 x 128 / 128 x 128, three of 4096 of 4096, 512 tokens 34 / 37; 128 x 192 / 128 x 128, three of 5003 of 3083, 333 tokens 33 / 42;
+// 128 x 128 / 256 x 128, 4096 of 4096, 1024 tokens 25 / 30; 64 x 128 / 128 x 128, 512 tokens 17 / 22; 64 x 64 / 64 x 128, 200 tokens 13 / 15; 64 x 32 / 64 x 64, three,
+// 24 tokens 14.5 / 15.0; 32 x 32 / 64 x 32, 64 tokens 8.8 / 11.9.  Teams: 64 x 64 with two 12.6, with one 17.8 (4096 of 4096, 64 tokens).
+template <int Y>
+int32_t many(W8Args &a, void *stream)
+{
+    constexpr struct {
+        int outputs, tokens;
+        float us;
+    } kShapes[] = {{256, 256, 1.7f}, {256, 192, 1.27f}, {256, 128, 0.95f}, {128, 192, 0.74f}, {128, 128, 0.56f}, {64, 128, 0.42f}, {64, 64, 0.3f}, {64, 32, 0.2f}, {32, 32, 0.18f}};
+    int best = 0;
+    float least = 0.0f;
+    for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
+        const float us = (float)rounds(parts(a, kShapes[i].outputs) * (((int64_t)a.T + kShapes[i].tokens - 1) / kShapes[i].tokens)) * kShapes[i].us;
+        if (i == 0 || us < least) {
+            best = i;
+            least = us;
+        }
+    }
+    switch (best) {
+    case 0: return launch_tile<1, 2, 4, 4, 2, Y>(a, stream);
+    case 1: return launch_tile<1, 4, 2, 2, 3, Y>(a, stream);
+    case 2: return launch_tile<1, 4, 2, 2, 2, Y>(a, stream);
+    case 3: return launch_tile<1, 4, 2, 1, 3, Y>(a, stream);
+    case 4: return launch_tile<1, 2, 2, 2, 2, Y>(a, stream);
+    case 5: return launch_tile<2, 2, 2, 1, 2, Y>(a, stream);
+    case 6: return launch_tile<2, 2, 2, 1, 1, Y>(a, stream);
+    case 7: return launch_tile<2, 2, 1, 1, 1, Y>(a, stream);
+    }
+    return launch_tile<4, 1, 1, 1, 1, Y>(a, stream);
 }
 
 } // namespace
@@ -396,11 +492,12 @@ int32_t launch_w8_pack(const slora_w8 *w, const int8_t *codes, const float *scal
 
 int32_t launch_w8(W8Args &a, int y, void *stream)
 {
+    auto by_tokens = [&](auto type) { return a.T <= 16 ? few<type.value>(a, stream) : many<type.value>(a, stream); };
     switch (y) {
-    case 0: return by_tokens<0>(a, stream);
-    case 1 + SLORA_F16: return by_tokens<1 + SLORA_F16>(a, stream);
+    case 0: return by_tokens(std::integral_constant<int, 0>{});
+    case 1 + SLORA_F16: return by_tokens(std::integral_constant<int, 1 + SLORA_F16>{});
     }
-    return by_tokens<1 + SLORA_BF16>(a, stream);
+    return by_tokens(std::integral_constant<int, 1 + SLORA_BF16>{});
 }
 
 } // namespace slora
