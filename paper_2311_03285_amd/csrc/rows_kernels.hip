@@ -40,6 +40,14 @@ struct Row {
     }
 };
 
+// The same row for a next pass, whose comparisons are made anew: kept from pass to pass they take more scalar registers than there are.
+template <int P, bool TAIL>
+__device__ __forceinline__ Row<P, TAIL> again(Row<P, TAIL> r)
+{
+    if constexpr (TAIL) asm volatile("" : "+v"(r.lane));
+    return r;
+}
+
 template <int DT>
 __device__ __forceinline__ void widen8(const u32x4 &raw, float (&v)[kPiece])
 {
@@ -64,8 +72,9 @@ __device__ __forceinline__ void load32(const Row<P, TAIL> &r, const float *from,
     }
 }
 template <int DT, int P, bool TAIL>
-__device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, const float (&v)[P][kPiece])
+__device__ __forceinline__ void store16(const Row<P, TAIL> &row, uint16_t *to, const float (&v)[P][kPiece])
 {
+    const Row<P, TAIL> r = again(row);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         if (!r.has(p)) continue;
@@ -85,8 +94,9 @@ __device__ __forceinline__ void store16(const Row<P, TAIL> &r, uint16_t *to, con
     }
 }
 template <int P, bool TAIL>
-__device__ __forceinline__ void store32(const Row<P, TAIL> &r, float *to, const float (&v)[P][kPiece])
+__device__ __forceinline__ void store32(const Row<P, TAIL> &row, float *to, const float (&v)[P][kPiece])
 {
+    const Row<P, TAIL> r = again(row);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         if (!r.has(p)) continue;
@@ -169,8 +179,9 @@ constexpr int kReductions = 11; // most of a row: two norms of five (mean, sprea
 __device__ __forceinline__ int magnitude(float v) { return (int)(__float_as_uint(v) & 0x7fffffffu); }
 
 template <int P, bool TAIL>
-__device__ __forceinline__ int largest(const Row<P, TAIL> &r, const float (&v)[P][kPiece], Team &team)
+__device__ __forceinline__ int largest(const Row<P, TAIL> &row, const float (&v)[P][kPiece], Team &team)
 {
+    const Row<P, TAIL> r = again(row);
     int top = 0;
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -188,8 +199,9 @@ struct Spread {
 // Layer norms: each wavefront's mean and its sum of squares about that, put together with one barrier: the squares about the row's mean are
 // those plus count * (difference of means)^2.  All terms are positive; nothing cancels.
 template <int P, bool TAIL>
-__device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (&v)[P][kPiece], bool layer, int width, Team &team)
+__device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &row, const float (&v)[P][kPiece], bool layer, int width, Team &team)
 {
+    Row<P, TAIL> r = again(row);
     Spread s{0.0f, 0.0f};
     if (layer) {
         float sum = 0.0f;
@@ -198,6 +210,7 @@ __device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &r, const float (
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) sum += r.valid(p, i) ? v[p][i] : 0.0f;
         s.mean = wave_sum(sum) / (float)max(r.count(team.waves == 1 ? 0 : team.wave), 1);
+        r = again(r);
     }
     float sum = 0.0f;
 #pragma unroll
@@ -286,9 +299,10 @@ __device__ __forceinline__ void affine(const Row<P, TAIL> &r, float (&v)[P][kPie
 // ---------------------------------------------------------------------------------------
 // Codes are rounded from fp32 values (not from the 16 bits that x is rounded to: one rounding, not two).
 template <int P, bool TAIL>
-__device__ __forceinline__ void store_codes(const Row<P, TAIL> &r, const RowsOut &out, int64_t t, const float (&v)[P][kPiece], Team &team)
+__device__ __forceinline__ void store_codes(const Row<P, TAIL> &row, const RowsOut &out, int64_t t, const float (&v)[P][kPiece], Team &team)
 {
-    const int top = largest(r, v, team);
+    const int top = largest(row, v, team);
+    const Row<P, TAIL> r = again(row);
     const bool spoiled = top >= 0x7f800000;
     const float a = fmaxf(__uint_as_float((uint32_t)top), kW8Least), inverse = spoiled ? 0.0f : 1.0f / a * 127.0f;
     int8_t *to = out.codes + t * out.codes_stride;
