@@ -528,7 +528,8 @@ typedef struct slora_w8 slora_w8;
  *   h' = h + scale * gate * b'
  *   x  = N(h'; pre_weight, pre_bias)
  *   N(v; w, c) = v / sqrt(mean(v^2) + eps) * w + c, or with SLORA_NORM_LAYER (v - mean(v)) / sqrt(var(v) + eps) * w + c
- * post_weight .. pre_bias: DEVICE vectors of `width` elements of `dtype`, 16-byte aligned, borrowed until slora_norm_destroy; a weight that is NULL
+ * post_weight .. pre_bias: DEVICE vectors of `width` elements of `dtype`, 16-byte aligned, borrowed until slora_norm_destroy (the 16 bytes that a vector ends in
+ * are read whole); a weight that is NULL
  * is 1, a bias that is NULL 0 (post ones without SLORA_NORM_POST: EINVAL).  1 <= width <= SLORA_NORM_MAX_WIDTH;
  * eps: 0, or at least 2^-60; scale finite.  SLORA_NORM_H32: the residual stream h is fp32, otherwise of `dtype`.
  * The junction belongs to the HIP device that is current.
@@ -578,11 +579,11 @@ int32_t slora_w8_destroy(slora_w8 *w);
 /*
  * y[k][t, o] = (sum_i x[k][t, i] * codes_k[o, i]) * x_scales[k][t] * scales_k[o] for n <= SLORA_MAX_MULTI matrices in one launch.
  * x[k]: DEVICE, T rows of w[k]'s inputs, 16-byte aligned, x_stride[k] bytes apart: a multiple of 16, at least inputs, at most 2^22; bytes up to
- * the next multiple of 16 behind a row are read and may hold anything.  x_scales[k]: DEVICE, T fp32, 4-byte aligned.  Entries of x and of x_scales may be equal.
+ * 128 behind a row are read, but not behind the last row's next multiple of 16, and may hold anything.  x_scales[k]: DEVICE, T fp32, 4-byte aligned.  Entries of x and of x_scales may be equal.
  * y[k]: DEVICE, 16-byte aligned, T rows of w[k]'s outputs, y_stride[k] >= outputs elements apart, fp32 or (_y16) of its 16-bit type,
  * written, not added to; nothing behind a row is written, and entries must not overlap.  x_stride, y_stride: HOST arrays.
  * Sums are whole numbers in 32 bits, exact in any order; each is rounded to fp32, multiplied by both scales there, and
- * rounded to y's type.  All matrices have one type and one device.  Allocates nothing; may be captured in a HIP graph.
+ * rounded to y's type.  All matrices have one type and one device; T is at most 2^30.  Allocates nothing; may be captured in a HIP graph.
  */
 int32_t slora_w8_matmul(int32_t n, const slora_w8 *const *w, const int8_t *const *x, const int64_t *x_stride, const float *const *x_scales,
                         int32_t T, float *const *y, const int64_t *y_stride, void *stream);

@@ -84,11 +84,13 @@ __device__ __forceinline__ void lds_barrier()
 
 // Few tokens: weights go from memory to the matrix instruction's registers.  A workgroup = RT tiles of 16 outputs and NT * 16 tokens; its
 // wavefronts take chunks of inputs in turn and are added up in LDS.
+// Bound: HBM and the time to fill it: four of 4096 of 4096, one token 11.3 us = 5.9 TB/s; two of 20480 of 5120, one token 32 us = 6.5 TB/s, 16 tokens 39 us.  With more
+// tokens every 16 outputs read all of x again: two of 20480 of 5120, 32 tokens 81 us with one tile, 55 with two, 42 from LDS below.
 constexpr int kFewWaves = 8;
 template <int RT, int NT, int Y>
 __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 {
-    constexpr int kAhead = 4; // chunks of weights under way
+    constexpr int kAhead = 4; // chunks under way
     __shared__ int part[kFewWaves][RT * NT][4][kWave];
     const W8Matrix &m = a.m[matrix_of(a, blockIdx.x)];
     const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
@@ -163,7 +165,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 // Rows of x come in eights of pieces (128 bytes); a row's place among 16 is permuted by the piece's number, so that the lanes that write
 // eights or sixteens of pieces are in different banks.
 // Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
-// to y in rows.
+// to y in rows.  (Straight from registers, 2 bytes a lane, 8192 tokens of 8192 x 8192 took 656 us where they take 519 this way, with the same loop.)
+// Bound, large products: power.  8192 tokens of 8192 x 8192 447 - 468 us = 2350 - 2460 TOP/s; the matrix units are busy for 74 % of the cycles, at 1.5 GHz of
+// 2.4.  (1676 TOP/s with operands read right before they are used, 2120 with reads spread by the compiler's groups, 2323 with one read, write or load
+// behind each product, 2420 with two wavefronts a SIMD instead of one.)  Small ones: what a compute unit reads for its tiles, and the stages' chain of barrier, LDS and
+// product: 512 tokens of 4096 x 4096 17 us, of which products at that rate take 8.  Between 17 and 100 tokens the weights' bytes: two of 20480 of 5120, 32 tokens 42 us = 5.0 TB/s.
 constexpr int kStageBytes = 2 * kW8Chunk;
 constexpr int kRaw = 0x00027000; // a buffer of 32-bit words, without a format
 constexpr int kNowhere = 1 << 30; // an offset behind every buffer's end: loads are 0
@@ -402,7 +408,7 @@ template <int RT, int NT, int Y>
 int32_t launch_few(W8Args &a, void *stream)
 {
     const int64_t groups = share_out(a, RT * kW8Rows, 1), blocks = ((int64_t)a.T + NT * 16 - 1) / (NT * 16);
-    if (groups * kFewWaves * kWave > kMostThreads || blocks > 65535) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", a.T);
+    if (groups * kFewWaves * kWave > kMostThreads || blocks > 65535) return fail(SLORA_ERANGE, "T=%d tokens of so many outputs are too many for one call", a.T);
     hipLaunchKernelGGL((w8_few_kernel<RT, NT, Y>), dim3((unsigned)groups, (unsigned)blocks), dim3(kFewWaves * kWave), 0, (hipStream_t)stream, a);
     return check_launch("w8_few");
 }
@@ -414,7 +420,7 @@ int32_t launch_tile(W8Args &a, void *stream)
     constexpr int kLds = Shape::lds(Y == 0 ? 4 : 2);
     static_assert(kLds <= 160 * 1024, "LDS");
     const int64_t groups = share_out(a, Shape::BO, ((int64_t)a.T + Shape::BT - 1) / Shape::BT);
-    if (groups * Shape::kThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens are too many for one call", a.T);
+    if (groups * Shape::kThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens of so many outputs are too many for one call", a.T);
     if (kLds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<TEAMS, WO, WT, MO, MT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
@@ -440,7 +446,7 @@ template <int Y>
 int32_t few(W8Args &a, void *stream)
 {
     const int64_t tiles = parts(a, kW8Rows);
-    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T)) return launch_few<1, 1, Y>(a, stream);
+    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T) && tiles * kFewWaves * kWave <= kMostThreads) return launch_few<1, 1, Y>(a, stream);
     return launch_few<2, 1, Y>(a, stream);
 }
 
@@ -454,14 +460,16 @@ template <int Y>
 int32_t many(W8Args &a, void *stream)
 {
     constexpr struct {
-        int outputs, tokens;
+        int outputs, tokens, threads;
         float us;
-    } kShapes[] = {{256, 256, 1.7f}, {256, 192, 1.27f}, {256, 128, 0.95f}, {128, 192, 0.74f}, {128, 128, 0.56f}, {64, 128, 0.42f}, {64, 64, 0.3f}, {64, 32, 0.2f}, {32, 32, 0.18f}};
+    } kShapes[] = {{256, 256, 512, 1.7f}, {256, 192, 512, 1.27f}, {256, 128, 512, 0.95f}, {128, 192, 512, 0.74f}, {128, 128, 256, 0.56f},
+                   {64, 128, 512, 0.42f}, {64, 64, 512, 0.3f},    {64, 32, 256, 0.2f},    {32, 32, 256, 0.18f}};
     int best = 0;
     float least = 0.0f;
     for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
-        const float us = (float)rounds(parts(a, kShapes[i].outputs) * (((int64_t)a.T + kShapes[i].tokens - 1) / kShapes[i].tokens)) * kShapes[i].us;
-        if (i == 0 || us < least) {
+        const int64_t groups = parts(a, kShapes[i].outputs) * (((int64_t)a.T + kShapes[i].tokens - 1) / kShapes[i].tokens);
+        const float us = (float)rounds(groups) * kShapes[i].us;
+        if (i == 0 || (us < least && groups * kShapes[i].threads <= kMostThreads)) {
             best = i;
             least = us;
         }
