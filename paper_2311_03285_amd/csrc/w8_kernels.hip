@@ -54,8 +54,6 @@ __global__ __launch_bounds__(256) void w8_pack_kernel(const int8_t *__restrict__
 __device__ __forceinline__ i32x4 mfma16(const i32x4 &a, const i32x4 &b, const i32x4 &c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ i32x16 mfma32(const i32x4 &a, const i32x4 &b, const i32x16 &c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 
-__device__ __forceinline__ i32x4 load16b(const int8_t *p) { return *reinterpret_cast<const i32x4 *>(p); }
-
 // Y: 0 fp32, else 1 + the 16-bit type.  The sum, exact so far, is rounded to fp32 and multiplied by both scales there; the product of the scales
 // alone could leave the range that the three have.
 __device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale) { return (float)sum * x_scale * w_scale; }
@@ -82,46 +80,40 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Few tokens: weights go from memory to the matrix instruction's registers.  A workgroup = RT tiles of 16 outputs and NT * 16 tokens; its
-// wavefronts take chunks of inputs in turn and are added up in LDS.
+// Up to 16 tokens: weights go from memory to the matrix instruction's registers.  A workgroup = RT tiles of 16 outputs; its wavefronts take chunks of inputs
+// in turn and are added up in LDS.
 // Bound: HBM and the time to fill it: four of 4096 of 4096, one token 11.3 us = 5.9 TB/s; two of 20480 of 5120, one token 32 us = 6.5 TB/s, 16 tokens 39 us.  With more
 // tokens every 16 outputs read all of x again: two of 20480 of 5120, 32 tokens 81 us with one tile, 55 with two, 42 from LDS below.
-constexpr int kFewWaves = 8;
-template <int RT, int NT, int Y>
+constexpr int kFewWaves = 8, kFewTokens = 16;
+template <int RT, int Y>
 __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 {
     constexpr int kAhead = 4; // chunks under way
-    __shared__ int part[kFewWaves][RT * NT][4][kWave];
+    __shared__ int part[kFewWaves][RT][4][kWave];
     const W8Matrix &m = a.m[matrix_of(a, blockIdx.x)];
     const int wave = wave_number(), lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
-    const int tile0 = ((int)blockIdx.x - m.first) * RT, t0 = blockIdx.y * NT * 16, chunks = m.chunks, x_last = m.x_last;
+    const int tile0 = ((int)blockIdx.x - m.first) * RT, chunks = m.chunks, x_last = m.x_last;
 
-    i32x4 sum[RT][NT];
+    i32x4 sum[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sum[r][t] = i32x4{0, 0, 0, 0};
-    const int8_t *row[NT], *codes[RT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) row[t] = m.x + (int64_t)min(t0 + t * 16 + n, a.T - 1) * m.x_stride;
+    for (int r = 0; r < RT; ++r) sum[r] = i32x4{0, 0, 0, 0};
+    // (tokens behind the last: the last once more, whose sums nobody takes)
+    const int8_t *const row = m.x + (int64_t)min(n, a.T - 1) * m.x_stride, *codes[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) codes[r] = m.codes + (int64_t)min(tile0 + r, m.tiles - 1) * chunks * kW8Block + lane * 16;
 
     struct Chunk {
-        i32x4 w[RT], x[NT];
+        i32x4 w[RT], x;
     } ring[kAhead];
     // (inputs behind the last: weights of 0)
     auto fetch = [&](Chunk &to, int c) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) to.w[r] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(codes[r] + (int64_t)c * kW8Block));
-#pragma unroll
-        for (int t = 0; t < NT; ++t) to.x[t] = load16b(row[t] + min(c * kW8Chunk + g * 16, x_last));
+        to.x = *reinterpret_cast<const i32x4 *>(row + min(c * kW8Chunk + g * 16, x_last));
     };
     auto work = [&](const Chunk &now) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sum[r][t] = mfma16(now.x[t], now.w[r], sum[r][t]);
+        for (int r = 0; r < RT; ++r) sum[r] = mfma16(now.x, now.w[r], sum[r]);
     };
     if (wave < chunks) {
         const int mine = (chunks - wave + kFewWaves - 1) / kFewWaves; // chunks of this wavefront
@@ -140,21 +132,19 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
         for (int k = 0; k < kAhead; ++k)
             if (i + k < mine) work(ring[k]);
     }
+    // token 4 g + i of output n is register i
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave][r * NT + t][i][lane] = sum[r][t][i];
+        for (int i = 0; i < 4; ++i) part[wave][r][i][lane] = sum[r][i];
     __syncthreads();
-    const int tokens = min(NT * 16, a.T - t0);
-    for (int w = threadIdx.x; w < RT * 16 * tokens; w += kFewWaves * kWave) {
-        const int r = w % (RT * 16), t = w / (RT * 16), o = tile0 * kW8Rows + r;
+    for (int w = threadIdx.x; w < RT * kW8Rows * a.T; w += kFewWaves * kWave) {
+        const int r = w % (RT * kW8Rows), t = w / (RT * kW8Rows), o = tile0 * kW8Rows + r;
         if (o >= m.outputs) continue;
         int total = 0;
 #pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) total += part[k][r / 16 * NT + t / 16][t % 4][t % 16 / 4 * 16 + r % 16];
-        store_y<Y>(m.y, (int64_t)(t0 + t) * m.y_stride + o, scaled(total, m.x_scales[t0 + t], m.scales[o]));
+        for (int k = 0; k < kFewWaves; ++k) total += part[k][r / 16][t % 4][t / 4 * 16 + r % 16];
+        store_y<Y>(m.y, (int64_t)t * m.y_stride + o, scaled(total, m.x_scales[t], m.scales[o]));
     }
 }
 
@@ -165,11 +155,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 // Rows of x come in eights of pieces (128 bytes); a row's place among 16 is permuted by the piece's number, so that the lanes that write
 // eights or sixteens of pieces are in different banks.
 // Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
-// to y in rows.  (Straight from registers, 2 bytes a lane, 8192 tokens of 8192 x 8192 took 656 us where they take 519 this way, with the same loop.)
+// to y in rows.
 // Bound, large products: power.  8192 tokens of 8192 x 8192 447 - 468 us = 2350 - 2460 TOP/s; the matrix units are busy for 74 % of the cycles, at 1.5 GHz of
-// 2.4.  (1676 TOP/s with operands read right before they are used, 2120 with reads spread by the compiler's groups, 2323 with one read, write or load
-// behind each product, 2420 with two wavefronts a SIMD instead of one.)  Small ones: what a compute unit reads for its tiles, and the stages' chain of barrier, LDS and
-// product: 512 tokens of 4096 x 4096 17 us, of which products at that rate take 8.  Between 17 and 100 tokens the weights' bytes: two of 20480 of 5120, 32 tokens 42 us = 5.0 TB/s.
+// 2.4.  (1676 TOP/s with operands read right before they are used and y stored from registers, 2120 with reads spread in groups and y through LDS, 2323 with
+// one read, write or load behind each product, 2420 with two wavefronts a SIMD instead of one.)  Small ones: the stages' chain of barrier, LDS and product; 512
+// tokens of 4096 x 4096 17 us, of which products at that rate take 8.  Between 17 and 100 tokens the weights' bytes: two of 20480 of 5120, 32 tokens 42 us = 5.0 TB/s.
 constexpr int kStageBytes = 2 * kW8Chunk;
 constexpr int kRaw = 0x00027000; // a buffer of 32-bit words, without a format
 constexpr int kNowhere = 1 << 30; // an offset behind every buffer's end: loads are 0
@@ -404,12 +394,12 @@ int64_t share_out(W8Args &a, int each, int64_t blocks)
     return groups;
 }
 
-template <int RT, int NT, int Y>
+template <int RT, int Y>
 int32_t launch_few(W8Args &a, void *stream)
 {
-    const int64_t groups = share_out(a, RT * kW8Rows, 1), blocks = ((int64_t)a.T + NT * 16 - 1) / (NT * 16);
-    if (groups * kFewWaves * kWave > kMostThreads || blocks > 65535) return fail(SLORA_ERANGE, "T=%d tokens of so many outputs are too many for one call", a.T);
-    hipLaunchKernelGGL((w8_few_kernel<RT, NT, Y>), dim3((unsigned)groups, (unsigned)blocks), dim3(kFewWaves * kWave), 0, (hipStream_t)stream, a);
+    const int64_t groups = share_out(a, RT * kW8Rows, 1);
+    if (groups * kFewWaves * kWave > kMostThreads) return fail(SLORA_ERANGE, "the matrices have too many outputs for one call");
+    hipLaunchKernelGGL((w8_few_kernel<RT, Y>), dim3((unsigned)groups), dim3(kFewWaves * kWave), 0, (hipStream_t)stream, a);
     return check_launch("w8_few");
 }
 
@@ -446,8 +436,8 @@ template <int Y>
 int32_t few(W8Args &a, void *stream)
 {
     const int64_t tiles = parts(a, kW8Rows);
-    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T) && tiles * kFewWaves * kWave <= kMostThreads) return launch_few<1, 1, Y>(a, stream);
-    return launch_few<2, 1, Y>(a, stream);
+    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T) && tiles * kFewWaves * kWave <= kMostThreads) return launch_few<1, Y>(a, stream);
+    return launch_few<2, Y>(a, stream);
 }
 
 // More tokens: the shape whose workgroups, of which compute units take rounds, are done first, by what a stage of one takes (measured with one and with
@@ -500,7 +490,7 @@ int32_t launch_w8_pack(const slora_w8 *w, const int8_t *codes, const float *scal
 
 int32_t launch_w8(W8Args &a, int y, void *stream)
 {
-    auto by_tokens = [&](auto type) { return a.T <= 16 ? few<type.value>(a, stream) : many<type.value>(a, stream); };
+    auto by_tokens = [&](auto type) { return a.T <= kFewTokens ? few<type.value>(a, stream) : many<type.value>(a, stream); };
     switch (y) {
     case 0: return by_tokens(std::integral_constant<int, 0>{});
     case 1 + SLORA_F16: return by_tokens(std::integral_constant<int, 1 + SLORA_F16>{});

@@ -82,6 +82,48 @@ def test_many_tokens_and_outputs(outputs, T):
     check([m], [x], run([m], [x], T, True))
 
 
+# Shapes of tiles: of (outputs, tokens), the one whose rounds over 256 compute units cost least.  These sizes take each of the nine, with ends in both directions.
+SHAPES = {(256, 256): (3900, 3500), (256, 192): (5100, 2000), (256, 128): (12250, 470), (128, 192): (15000, 333), (128, 128): (4090, 1000), (64, 128): (4090, 500),
+          (64, 64): (4090, 200), (64, 32): (12280, 23), (32, 32): (4090, 63)}
+
+
+@pytest.mark.parametrize("y16", [False, True])
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_every_shape_of_tiles(shape, y16):
+    outputs, T = SHAPES[shape]
+    cost = {(256, 256): 1.7, (256, 192): 1.27, (256, 128): 0.95, (128, 192): 0.74, (128, 128): 0.56, (64, 128): 0.42, (64, 64): 0.3, (64, 32): 0.2, (32, 32): 0.18}
+    took = min(cost, key=lambda s: -(-(-(-outputs // s[0]) * -(-T // s[1])) // 256) * cost[s])
+    assert took == shape
+    for more, pad in ((0, 0), (3, 0), (3, 6)):  # rows 16 bytes apart that end so or between, and rows that are not
+        m = Matrix(outputs // 8 * 8 + more, 390, outputs)
+        x = X(T, 390, 6, pad=16)
+        check([m], [x], run([m], [x], T, y16, y_pad=-m.shape[0] % 8 + pad))
+
+
+def test_graphs_on_two_streams_at_once():
+    """nothing is shared between calls"""
+    sets = [(Matrix(600 + 50 * i, 1500, i, "bf16"), X(T, 1500, i)) for i, T in enumerate((1, 40, 130, 500))]
+    graphs, streams, ys = [], [], []
+    for m, x in sets:
+        T = len(x.codes)
+        y, graph, stream = torch.zeros(T, m.shape[0], device="cuda"), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=stream):
+            slora.w8_matmul([m.handle], [x.d_codes.data_ptr()], [x.stride], [x.d_scales.data_ptr()], T, [y.data_ptr()], [m.shape[0]], torch.cuda.current_stream())
+        graphs.append(graph)
+        streams.append(stream)
+        ys.append(y)
+    for _ in range(4):
+        for y in ys:
+            y.zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (m, x), y in zip(sets, ys):
+            check([m], [x], [y])
+
+
 @pytest.mark.parametrize("T", [1, 40, 70, 300])
 def test_matrices_of_different_shapes(T):
     shapes = [(16, 64), (100, 8), (3, 2048), (512, 512), (31, 136), (64, 64), (1, 1000), (40, 3200)]
