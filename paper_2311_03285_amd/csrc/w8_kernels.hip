@@ -186,6 +186,9 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
     constexpr int BO = Shape::BO, BT = Shape::BT, kUnits = Shape::kUnits, kTeam = Shape::kTeam;
     constexpr int kPutsX = BT * kUnits / kTeam, kPutsW = BO * kUnits / kTeam, kPuts = kPutsX + kPutsW; // units of a thread and stage
     constexpr int kReads = MT + MO;
+    // Weights that few tiles of tokens read are loaded without a place in the caches (bit 1).  us with / without: two of 20480 of 5120, 32 tokens 38.4 / 42.2, 100 tokens 45.5 /
+    // 48.1; three of 4096 of 4096, 24 tokens 13.2 / 14.5; 4096 of 4096, 512 tokens 16.7 / 17.2; with the largest shapes, two of 20480 of 5120, 2048 tokens 395 / 381.
+    constexpr int kOnce = BO * BT <= 256 * 128 ? 2 : 0;
     extern __shared__ i32x4 lds[]; // [team] {[2][BT * kUnits], [2][BO * kUnits]}
     const int k = matrix_of(a, blockIdx.x);
     const W8Matrix &m = a.m[k];
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
         if (j < kPutsX)
             raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x_rows, at[j] + (number < stages ? number * kStageBytes : kNowhere), 0, 0));
         else
-            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j] + (number < stages ? number * (2 * kW8Block) : kNowhere), 0, 0));
+            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j] + (number < stages ? number * (2 * kW8Block) : kNowhere), 0, kOnce));
     };
     auto put = [&](int j, int buffer) {
         if (j < kPutsX)
