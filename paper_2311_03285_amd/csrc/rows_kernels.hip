@@ -55,8 +55,8 @@ __device__ __forceinline__ void widen8(const u32x4 &raw, float (&v)[kPiece])
     for (int i = 0; i < kPiece; ++i) v[i] = widen<DT>((uint16_t)(raw[i / 2] >> (16 * (i % 2))));
 }
 
-// Rows, which are read once, are loaded without a place in the caches (once), vectors that all rows read with one.  us with / without: gated 2048 rows of 20480 42 / 48, 4096 rows
-// of 5120 to 8 bits 14 / 15.3; with the vectors as well, norms of 8192 rows of 8192 121 / 96.
+// ONCE: rows are loaded without a place in the caches (vectors that all rows read always with one).  us with / without, of rows that are in none: gated 3001 rows of 13007 40 / 44, 8192 rows of
+// 4096 through a norm 44.5 / 48.7; of rows that are in the memory-side cache: 4096 of 5120 to 8 bits 13.6 / 12.1, norms of 777 of 5003 18.4 / 15.1.
 template <bool ONCE, typename T>
 __device__ __forceinline__ T load_piece(const T *from)
 {
@@ -73,13 +73,13 @@ __device__ __forceinline__ void load16(const Row<P, TAIL> &r, const uint16_t *fr
 #pragma unroll
     for (int p = 0; p < P; ++p) raw[p] = load_piece<ONCE>(reinterpret_cast<const u32x4 *>(from + r.at(p)));
 }
-template <int P, bool TAIL>
+template <bool ONCE, int P, bool TAIL>
 __device__ __forceinline__ void load32(const Row<P, TAIL> &r, const float *from, f32x4 (&raw)[P][2])
 {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        raw[p][0] = load_piece<true>(reinterpret_cast<const f32x4 *>(from + r.at(p)));
-        raw[p][1] = load_piece<true>(reinterpret_cast<const f32x4 *>(from + (TAIL ? min(r.at(p) + 4, (r.width - 1) / 4 * 4) : r.at(p) + 4)));
+        raw[p][0] = load_piece<ONCE>(reinterpret_cast<const f32x4 *>(from + r.at(p)));
+        raw[p][1] = load_piece<ONCE>(reinterpret_cast<const f32x4 *>(from + (TAIL ? min(r.at(p) + 4, (r.width - 1) / 4 * 4) : r.at(p) + 4)));
     }
 }
 template <int DT, int P, bool TAIL>
@@ -358,8 +358,8 @@ __device__ __forceinline__ int64_t row_number(int waves, int wave)
 
 // One row for the workgroup, or (waves == 1) one for each of its wavefronts.
 // Bound: HBM where there are rows enough (8192 rows of 8192, a norm behind the block and a gate by channel, 537 MB: 97 us = 5.5 TB/s, a copy reaches 5.05; 2048
-// of 4096 14.9 us = 4.5 TB/s); below, the chain of two loads, two to four reductions and a store (777 rows of 5003 in fp32, gate by token: 20 us = 2.7 TB/s), and the launch (one row 6.5 us).
-template <int DT, bool H32, int P, bool TAIL>
+// of 4096 14.9 us = 4.5 TB/s); below, the chain of two loads, two to four reductions and a store (777 rows of 5003 in fp32, gate by token: 15 us = 3.6 TB/s), and the launch (one row 6.5 us).
+template <int DT, bool H32, int P, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves)
 {
     __shared__ uint32_t slots[kReductions][kRowThreads / kWave];
@@ -380,9 +380,9 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
     Raw h;
     auto load_h = [&] {
         if constexpr (H32)
-            load32(r, static_cast<const float *>(a.h) + t * a.h_stride, h);
+            load32<ONCE>(r, static_cast<const float *>(a.h) + t * a.h_stride, h);
         else
-            load16<true>(r, static_cast<const uint16_t *>(a.h) + t * a.h_stride, h);
+            load16<ONCE>(r, static_cast<const uint16_t *>(a.h) + t * a.h_stride, h);
     };
     if constexpr (kAhead) load_h();
     if (a.block) {
@@ -391,10 +391,10 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
             if (a.post && a.post_weight) load16<false>(r, a.post_weight, weight);
         };
         auto load_gate = [&] {
-            if (a.gate && a.gate_stride) load16<true>(r, a.gate + t * a.gate_stride, gate);
+            if (a.gate && a.gate_stride) load16<ONCE>(r, a.gate + t * a.gate_stride, gate);
             if (a.gate && !a.gate_stride) load16<false>(r, a.gate, gate);
         };
-        load16<true>(r, a.block + t * a.block_stride, raw);
+        load16<ONCE>(r, a.block + t * a.block_stride, raw);
         if constexpr (kAhead) load_weight();
         if constexpr (kAhead) load_gate();
 #pragma unroll
@@ -453,8 +453,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves
 
 // ... as above.  exp and 1 / (1 + exp) are the hardware's, good to a step each (with expf and a division, which are longer than the row takes to load, 3001
 // rows of 13007 took 62 us); where exp(-u) leaves fp32's range (u < -88) or 1 + exp(-u) passes 2^126, the product is 0.
-// Bound: HBM (3001 gated rows of 13007, 234 MB: 44 us = 5.3 TB/s; 4096 rows of 5120 to 8 bits, 63 MB: 15 us = 4.2 TB/s).
-template <int DT, int P, bool TAIL>
+// Bound: HBM (3001 gated rows of 13007, 234 MB: 40 us = 5.9 TB/s; 4096 rows of 5120 to 8 bits, 63 MB: 12.1 us = 5.2 TB/s).
+template <int DT, int P, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, int waves)
 {
     __shared__ uint32_t slots[1][kRowThreads / kWave];
@@ -464,8 +464,8 @@ __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, i
     const Row<P, TAIL> r = row_of<P, TAIL>(a.width, waves);
     Team team{slots, waves, wave};
     u32x4 raw[P], gate[P];
-    load16<true>(r, a.x + t * a.x_stride, raw);
-    if (a.gate) load16<true>(r, a.gate + t * a.gate_stride, gate);
+    load16<ONCE>(r, a.x + t * a.x_stride, raw);
+    if (a.gate) load16<ONCE>(r, a.gate + t * a.gate_stride, gate);
     float v[P][kPiece];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -524,15 +524,18 @@ int32_t by_flag(bool flag, F f)
 
 int32_t launch_norm(const NormArgs &a, int32_t dtype, bool h32, void *stream)
 {
+    const int64_t bytes = (int64_t)a.T * a.width * ((h32 ? 4 : 2) + (a.block ? 2 : 0) + (a.gate && a.gate_stride ? 2 : 0)); // of rows
     return by_width<4>(a.width, [&](auto p, int waves) {
         return by_flag(a.width % kPiece != 0, [&](auto tail) {
             return by_flag(h32, [&](auto h) {
-                const Grid g(a.T, waves);
-                if (dtype == SLORA_F16)
-                    hipLaunchKernelGGL((norm_kernel<SLORA_F16, h.value, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-                else
-                    hipLaunchKernelGGL((norm_kernel<SLORA_BF16, h.value, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-                return check_launch("norm");
+                return by_flag(bytes >= kOnceBytes, [&](auto once) {
+                    const Grid g(a.T, waves);
+                    if (dtype == SLORA_F16)
+                        hipLaunchKernelGGL((norm_kernel<SLORA_F16, h.value, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                    else
+                        hipLaunchKernelGGL((norm_kernel<SLORA_BF16, h.value, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                    return check_launch("norm");
+                });
             });
         });
     });
@@ -540,14 +543,17 @@ int32_t launch_norm(const NormArgs &a, int32_t dtype, bool h32, void *stream)
 
 int32_t launch_quantize(const QuantizeArgs &a, int32_t dtype, void *stream)
 {
+    const int64_t bytes = (int64_t)a.T * a.width * (a.gate ? 4 : 2);
     return by_width<8>(a.width, [&](auto p, int waves) {
         return by_flag(a.width % kPiece != 0, [&](auto tail) {
-            const Grid g(a.T, waves);
-            if (dtype == SLORA_F16)
-                hipLaunchKernelGGL((quantize_kernel<SLORA_F16, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-            else
-                hipLaunchKernelGGL((quantize_kernel<SLORA_BF16, p.value, tail.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-            return check_launch("quantize");
+            return by_flag(bytes >= kOnceBytes, [&](auto once) {
+                const Grid g(a.T, waves);
+                if (dtype == SLORA_F16)
+                    hipLaunchKernelGGL((quantize_kernel<SLORA_F16, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                else
+                    hipLaunchKernelGGL((quantize_kernel<SLORA_BF16, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                return check_launch("quantize");
+            });
         });
     });
 }

@@ -156,12 +156,13 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
 // eights or sixteens of pieces are in different banks.
 // Outputs are the rows of the matrix instruction here, so that a lane has four neighbouring ones of a token, which go to LDS together and from there
 // to y in rows.
-// Bound, large products: power.  8192 tokens of 8192 x 8192 447 - 468 us = 2350 - 2460 TOP/s; the matrix units are busy for 74 % of the cycles, at 1.5 GHz of
+// Bound, large products: power.  8192 tokens of 8192 x 8192 439 - 476 us by the card = 2310 - 2500 TOP/s; the matrix units are busy for 74 % of the cycles, at 1.5 GHz of
 // 2.4.  (1676 TOP/s with operands read right before they are used and y stored from registers, 2120 with reads spread in groups and y through LDS, 2323 with
 // one read, write or load behind each product, 2420 with two wavefronts a SIMD instead of one.)  Small ones: the stages' chain of barrier, LDS and product; 512
-// tokens of 4096 x 4096 17 us, of which products at that rate take 8.  Between 17 and 100 tokens the weights' bytes: two of 20480 of 5120, 32 tokens 42 us = 5.0 TB/s.
+// tokens of 4096 x 4096 17 us, of which products at that rate take 8.  Between 17 and 100 tokens the weights' bytes: two of 20480 of 5120, 32 tokens 38 us = 5.6 TB/s.
 constexpr int kStageBytes = 2 * kW8Chunk;
 constexpr int kRaw = 0x00027000; // a buffer of 32-bit words, without a format
+// ONCE: weights are loaded without a place in the caches (bit 1 of a load's last argument).
 constexpr int kNowhere = 1 << 30; // an offset behind every buffer's end: loads are 0
 
 template <int TEAMS, int WO, int WT, int MO, int MT>
@@ -179,16 +180,13 @@ struct Tile {
 // wavefronts of a SIMD: with 144 sums a lane and more there is one
 constexpr int tile_occupancy(int blocks) { return blocks >= 8 ? 1 : 2; }
 
-template <int TEAMS, int WO, int WT, int MO, int MT, int Y>
+template <int TEAMS, int WO, int WT, int MO, int MT, bool ONCE, int Y>
 __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void w8_tile_kernel(W8Args a)
 {
     typedef Tile<TEAMS, WO, WT, MO, MT> Shape;
     constexpr int BO = Shape::BO, BT = Shape::BT, kUnits = Shape::kUnits, kTeam = Shape::kTeam;
     constexpr int kPutsX = BT * kUnits / kTeam, kPutsW = BO * kUnits / kTeam, kPuts = kPutsX + kPutsW; // units of a thread and stage
     constexpr int kReads = MT + MO;
-    // Weights that few tiles of tokens read are loaded without a place in the caches (bit 1).  us with / without: two of 20480 of 5120, 32 tokens 38.4 / 42.2, 100 tokens 45.5 /
-    // 48.1; three of 4096 of 4096, 24 tokens 13.2 / 14.5; 4096 of 4096, 512 tokens 16.7 / 17.2; with the largest shapes, two of 20480 of 5120, 2048 tokens 395 / 381.
-    constexpr int kOnce = BO * BT <= 256 * 128 ? 2 : 0;
     extern __shared__ i32x4 lds[]; // [team] {[2][BT * kUnits], [2][BO * kUnits]}
     const int k = matrix_of(a, blockIdx.x);
     const W8Matrix &m = a.m[k];
@@ -226,7 +224,7 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
         if (j < kPutsX)
             raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x_rows, at[j] + (number < stages ? number * kStageBytes : kNowhere), 0, 0));
         else
-            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j] + (number < stages ? number * (2 * kW8Block) : kNowhere), 0, kOnce));
+            raw[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_tiles, at[j] + (number < stages ? number * (2 * kW8Block) : kNowhere), 0, ONCE ? 2 : 0));
     };
     auto put = [&](int j, int buffer) {
         if (j < kPutsX)
@@ -406,7 +404,7 @@ int32_t launch_few(W8Args &a, void *stream)
     return check_launch("w8_few");
 }
 
-template <int TEAMS, int WO, int WT, int MO, int MT, int Y>
+template <int TEAMS, int WO, int WT, int MO, int MT, bool ONCE, int Y>
 int32_t launch_tile(W8Args &a, void *stream)
 {
     typedef Tile<TEAMS, WO, WT, MO, MT> Shape;
@@ -415,10 +413,10 @@ int32_t launch_tile(W8Args &a, void *stream)
     const int64_t groups = share_out(a, Shape::BO, ((int64_t)a.T + Shape::BT - 1) / Shape::BT);
     if (groups * Shape::kThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens of so many outputs are too many for one call", a.T);
     if (kLds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<TEAMS, WO, WT, MO, MT, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&w8_tile_kernel<TEAMS, WO, WT, MO, MT, ONCE, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess) return fail(SLORA_EHIP, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
     }
-    hipLaunchKernelGGL((w8_tile_kernel<TEAMS, WO, WT, MO, MT, Y>), dim3((unsigned)groups), dim3(Shape::kThreads), kLds, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((w8_tile_kernel<TEAMS, WO, WT, MO, MT, ONCE, Y>), dim3((unsigned)groups), dim3(Shape::kThreads), kLds, (hipStream_t)stream, a);
     return check_launch("w8_tile");
 }
 
@@ -467,17 +465,23 @@ int32_t many(W8Args &a, void *stream)
             least = us;
         }
     }
+    // The weights of large calls are loaded once each, but by the largest shapes, whose tiles of tokens share them.  us with / without, inputs that are not in any cache: two of 20480
+    // of 5120, 32 tokens 38.2 / 42.3, 100 tokens 45.5 / 48.1; four of 4096 of 4096, 128 tokens 19.6 / 21.7; two of 20480 of 5120, 2048 tokens (256 x 256) 395 / 381.
+    // Of 50 MB that are in the memory-side cache: three of 4096 of 4096, 24 tokens behind a norm 19.2 / 17.5.
+    int64_t bytes = 0;
+    for (int32_t k = 0; k < a.n; ++k) bytes += (int64_t)a.m[k].tiles * a.m[k].chunks * kW8Block;
+    auto by_once = [&](auto launch) { return bytes >= kOnceBytes ? launch(std::true_type{}) : launch(std::false_type{}); };
     switch (best) {
-    case 0: return launch_tile<1, 2, 4, 4, 2, Y>(a, stream);
-    case 1: return launch_tile<1, 4, 2, 2, 3, Y>(a, stream);
-    case 2: return launch_tile<1, 4, 2, 2, 2, Y>(a, stream);
-    case 3: return launch_tile<1, 4, 2, 1, 3, Y>(a, stream);
-    case 4: return launch_tile<1, 2, 2, 2, 2, Y>(a, stream);
-    case 5: return launch_tile<2, 2, 2, 1, 2, Y>(a, stream);
-    case 6: return launch_tile<2, 2, 2, 1, 1, Y>(a, stream);
-    case 7: return launch_tile<2, 2, 1, 1, 1, Y>(a, stream);
+    case 0: return launch_tile<1, 2, 4, 4, 2, false, Y>(a, stream);
+    case 1: return launch_tile<1, 4, 2, 2, 3, false, Y>(a, stream);
+    case 2: return by_once([&](auto once) { return launch_tile<1, 4, 2, 2, 2, once.value, Y>(a, stream); });
+    case 3: return by_once([&](auto once) { return launch_tile<1, 4, 2, 1, 3, once.value, Y>(a, stream); });
+    case 4: return by_once([&](auto once) { return launch_tile<1, 2, 2, 2, 2, once.value, Y>(a, stream); });
+    case 5: return by_once([&](auto once) { return launch_tile<2, 2, 2, 1, 2, once.value, Y>(a, stream); });
+    case 6: return by_once([&](auto once) { return launch_tile<2, 2, 2, 1, 1, once.value, Y>(a, stream); });
+    case 7: return by_once([&](auto once) { return launch_tile<2, 2, 1, 1, 1, once.value, Y>(a, stream); });
     }
-    return launch_tile<4, 1, 1, 1, 1, Y>(a, stream);
+    return by_once([&](auto once) { return launch_tile<4, 1, 1, 1, 1, once.value, Y>(a, stream); });
 }
 
 } // namespace

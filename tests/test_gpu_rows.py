@@ -323,6 +323,35 @@ def test_rows_behind_4_GiB_and_more_rows_than_a_grid_is_wide():
         assert np.array_equal(codes[t:t + 1, :width].cpu().numpy(), want) and scales[t].item() == by[0]
 
 
+@pytest.mark.parametrize("width", [100, 515, 1000, 1003, 4096, 5003, 20000, 20005])
+def test_rows_too_large_for_the_caches(width):
+    """from 64 MiB of them on, other loads: every row as in a call of few"""
+    T, t = (70 << 20) // (4 * width) + 1, torch.bfloat16
+    some = [0, 1, T // 2, T - 1]
+    for h32 in (False, True):
+        m = Norm(width, "bf16", layer=h32, post=True, bias=True, h32=h32)
+        h, block = rows(T, width, torch.float32 if h32 else t, 1), rows(T, width, t, 2)
+        whole, few = m(h, block), m(h[some].contiguous(), block[some].contiguous())
+        for name in few:
+            assert torch.equal(whole[name][some], few[name]), name
+    for gate in (None, block):
+        kw = {} if gate is None else dict(gate=gate.data_ptr(), gate_stride=gate.stride(0))
+        x, kind = (block, slora.ACT_NONE) if gate is None else (whole["x"].contiguous() if width % 8 == 0 else block, slora.ACT_SILU)
+        x = torch.cat([x, x]) if gate is None else x
+        n, out = x.shape[0], {}
+        for which in ("whole", "few"):
+            pick = list(range(n)) if which == "whole" else some
+            a = x if which == "whole" else x[some].contiguous()
+            g = gate if which == "whole" or gate is None else gate[some].contiguous()
+            if g is not None:
+                kw = dict(gate=g.data_ptr(), gate_stride=g.stride(0))
+            codes, scales = torch.empty((len(pick), -(-width // 16) * 16), dtype=torch.int8, device="cuda"), torch.empty(len(pick), device="cuda")
+            slora.w8_quantize(len(pick), width, slora.BF16, kind, a.data_ptr(), a.stride(0), codes=codes.data_ptr(), codes_stride=codes.stride(0), scales=scales.data_ptr(), **kw)
+            torch.cuda.synchronize()
+            out[which] = codes[:, :width], scales
+        assert torch.equal(out["whole"][0][some], out["few"][0]) and torch.equal(out["whole"][1][some], out["few"][1])
+
+
 def test_no_tokens():
     m = Norm(64, "f16")
     slora.norm_apply(m.handle, 0, 0, 0)

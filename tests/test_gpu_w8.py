@@ -100,6 +100,17 @@ def test_every_shape_of_tiles(shape, y16):
         check([m], [x], run([m], [x], T, y16, y_pad=-m.shape[0] % 8 + pad))
 
 
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_weights_too_large_for_the_caches(shape):
+    """from 64 MiB of them on, other loads; a few tokens and the last ones are checked"""
+    outputs, T = SHAPES[shape]
+    inputs = -(-(68 << 20) // outputs)
+    m, x = Matrix(outputs, inputs, 3), X(T, inputs, 4)
+    y = run([m], [x], T, False)[0]
+    rows = sorted({0, 1, T // 3, T // 2, T - 2, T - 1})
+    within(y[rows], *product(x.codes[rows], x.scales[rows], m.codes, m.scales))
+
+
 def test_graphs_on_two_streams_at_once():
     """nothing is shared between calls"""
     sets = [(Matrix(600 + 50 * i, 1500, i, "bf16"), X(T, 1500, i)) for i, T in enumerate((1, 40, 130, 500))]

@@ -38,8 +38,8 @@ def test_wavefronts(tmp_path):
         assert waves >= 4, (name, waves)
     seen = 0
     for name, waves in occupancy("w8_kernels.hip", tmp_path).items():
-        m = re.search(r"w8_tile_kernelILi(\d)ELi(\d)ELi(\d)ELi(\d)ELi(\d)E", name)
+        m = re.search(r"w8_tile_kernelILi(\d)ELi(\d)ELi(\d)ELi(\d)ELi(\d)ELb[01]E", name)
         if m:
             seen += 1
             assert waves >= (2 if int(m.group(4)) * int(m.group(5)) >= 6 else 3), (name, waves)
-    assert seen == 27
+    assert seen == 48
