@@ -55,6 +55,8 @@ class AttentionLayer:
         self.cache = slora.kv8_init(self.pool, layers, n_heads, n_heads, self.D, max_seqs, max_tokens, self.exps.data_ptr())
         self.weights = [torch.zeros((max_seqs, n_heads, max_tokens), device=device) for _ in range(layers)]
         self.pos = [torch.zeros((max_seqs, n_heads, max_tokens), dtype=torch.int32, device=device) for _ in range(layers)]
+        # Packing and uploads run on torch's stream, behind the operations there that make what they read.
+        stream = torch.cuda.current_stream()
         # base weights: codes about 8, a scale per group; slot 4 * layer + (0, 1, 2, 3) is q, k, v, o, for LoRA as well
         self.codes, self.scales, self.packed, self.matrices, self.norms = [], [], [], [], []
         for _ in range(4 * layers if bits == 4 else 0):
@@ -62,13 +64,13 @@ class AttentionLayer:
             s = ((0.5 + torch.rand((H, -(-H // group)), device=device, generator=g)) / (2.6 * H ** 0.5)).to(self.dtype)
             packed = torch.empty(slora.w4_bytes(H, H, group), dtype=torch.uint8, device=device)
             nibbles = (c[:, 0::2] | (c[:, 1::2] << 4)).contiguous()
-            self.matrices.append(slora.w4_pack(H, H, group, dtype, nibbles.data_ptr(), s.data_ptr(), None, packed.data_ptr()))
+            self.matrices.append(slora.w4_pack(H, H, group, dtype, nibbles.data_ptr(), s.data_ptr(), None, packed.data_ptr(), stream))
             self.codes.append(c)
             self.scales.append(s)
             self.packed.append(packed)
             torch.cuda.synchronize()  # (nibbles may go)
         if bits == 8:
-            self._weights_of_8_bits(g)
+            self._weights_of_8_bits(g, stream)
         self.group = group
         self.adapters: Dict[int, torch.Tensor] = {}
         for a, r in ranks.items():
@@ -77,9 +79,10 @@ class AttentionLayer:
             w[:, 0] /= H ** 0.5
             w[:, 1] /= 4 * r ** 0.5
             self.adapters[a] = w.to(self.dtype)
-            slora.adapter_upload(self.pool, a, self.adapters[a].data_ptr())
+            slora.adapter_upload(self.pool, a, self.adapters[a].data_ptr(), stream)
+        torch.cuda.synchronize()  # (steps may run on another stream)
 
-    def _weights_of_8_bits(self, g) -> None:
+    def _weights_of_8_bits(self, g, stream) -> None:
         """... as above, and behind them gate, up and down of each layer; a norm before each half of a layer, and one that adds the last block"""
         H, wide, layers, device = self.H, self.wide, self.layers, self.pages.device
         shapes = [(H, H)] * (4 * layers) + ([(wide, H), (wide, H), (H, wide)] * layers if wide else [])
@@ -87,10 +90,10 @@ class AttentionLayer:
             self.codes.append((torch.randn((outputs, inputs), device=device, generator=g) * 35).round_().clamp_(-127, 127).to(torch.int8))
             self.scales.append((0.5 + torch.rand((outputs,), device=device, generator=g)) / (35 * inputs ** 0.5))
             self.packed.append(torch.empty(slora.w8_bytes(outputs, inputs), dtype=torch.uint8, device=device))
-            self.matrices.append(slora.w8_pack(outputs, inputs, self.lib_dtype, self.codes[-1].data_ptr(), self.scales[-1].data_ptr(), self.packed[-1].data_ptr()))
+            self.matrices.append(slora.w8_pack(outputs, inputs, self.lib_dtype, self.codes[-1].data_ptr(), self.scales[-1].data_ptr(), self.packed[-1].data_ptr(),
+                                               stream))
         self.norm_weights = [(1 + 0.2 * torch.randn((H,), device=device, generator=g)).to(self.dtype) for _ in range((2 if wide else 1) * layers)]
         self.norms = [slora.norm_init(H, self.lib_dtype, pre_weight=w.data_ptr()) for w in self.norm_weights] + [slora.norm_init(H, self.lib_dtype)]
-        torch.cuda.synchronize()
 
     def step(self, seqs: Sequence[int], tokens: Sequence[int], adapters: Sequence[int], x: torch.Tensor) -> List[torch.Tensor]:
         """x: [sum of tokens, H], new tokens of `seqs` (whose adapters are given); returns every layer's output, each layer reading the one before.
