@@ -45,6 +45,8 @@ class AttentionLayer:
                  group: int = 128, dtype: int = slora.F16, seed: int = 0, device="cuda", bits: int = 4, wide: int = 0):
         if bits not in (4, 8) or wide < 0 or (wide and bits == 4):
             raise ValueError("bits must be 4 or 8, and a feed-forward block needs 8")
+        if bits == 8 and (H > slora.NORM_MAX_WIDTH or wide > slora.W8_MAX_WIDTH):
+            raise ValueError(f"norms are of rows up to {slora.NORM_MAX_WIDTH} wide, gated products up to {slora.W8_MAX_WIDTH}")
         self.bits, self.wide, self.lib_dtype = bits, wide, dtype
         self.H, self.n_heads, self.D, self.layers, self.budget, self.recent, self.dtype = H, n_heads, H // n_heads, layers, budget, recent, DTYPES[dtype]
         g = torch.Generator(device=device)

@@ -21,6 +21,7 @@ PLAN_INFO_N = 13
 POOL_STATS_N = 4
 KV8_INFO_N = 4
 NORM_LAYER, NORM_POST, NORM_H32 = 1, 2, 4
+NORM_MAX_WIDTH, W8_MAX_WIDTH = 32768, 65536
 ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
 PLAN_INFO_KEYS = ("tokens", "groups", "groups_vec", "groups_mfma", "vec_shrink_items", "vec_expand_items",
                   "mfma_shrink_items", "mfma_expand_items", "v_stride", "sum_rank", "split_tiles",

@@ -42,3 +42,25 @@ def test_weights_are_laid_out_behind_the_operations_that_make_them(calls, bits, 
     assert [name for name, _ in enqueued] == [f"w{bits}_pack"] * matrices + ["adapter_upload"] * 2
     assert all(stream is Stream for _, stream in enqueued)
     assert calls[-1][0] == "wait"  # what a step on another stream reads is there
+
+
+@pytest.mark.parametrize("kw", [dict(wide=65537), dict(wide=70000), dict(wide=131071), dict(H=32832, n_heads=8), dict(H=65536, n_heads=8)])
+def test_layers_that_no_step_could_run_are_refused_when_built(calls, kw):
+    """rows of the gated product and of the norms are wider than those operators take; products alone would take them, so that a step would fail midway"""
+    with pytest.raises(ValueError, match="wide"):
+        AttentionLayer(**{**SIZES, **kw}, bits=8)
+    assert not calls
+
+
+def test_the_widest_rows_are_those_that_the_operators_take():
+    for width, refused in ((slora.W8_MAX_WIDTH, False), (slora.W8_MAX_WIDTH + 1, True)):
+        if refused:
+            with pytest.raises(slora.SloraError, match="width"):
+                slora.w8_quantize(0, width, slora.F16, slora.ACT_NONE, 0, 0)
+        else:
+            slora.w8_quantize(0, width, slora.F16, slora.ACT_NONE, 0, 0)
+    with pytest.raises(slora.SloraError, match="width"):
+        slora.norm_init(slora.NORM_MAX_WIDTH + 1, slora.F16)
+    with pytest.raises(slora.SloraError) as e:  # (without a GPU it is the device that is missed)
+        slora.norm_apply(slora.norm_init(slora.NORM_MAX_WIDTH, slora.F16), -1, 0, 0)
+    assert e.value.code in (slora.EHIP, slora.EINVAL) and "width" not in str(e.value)
