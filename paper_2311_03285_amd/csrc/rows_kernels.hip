@@ -251,7 +251,8 @@ __device__ __forceinline__ Spread spread_of(const Row<P, TAIL> &row, const float
 
 // v = (v - mean) / sqrt(mean square + eps), with all of the row in registers: the spread is of differences, not a difference of sums.
 // Squares that leave fp32's range (bfloat16 and fp32 rows can) are taken again of v times a power of two, which is
-// exact; eps, which is 0 or at least 2^-60, is then 0 or negligible or scaled along.  All lanes of the row go the same way.
+// exact; eps, which is 0 or at least 2^-60, is scaled along.  With an eps, squares are never too small, and rows are only scaled down; what is left of eps is then far
+// below any spread but 0, and must not become 0 itself: a layer norm of equal values is 0, however large they are.  All lanes of the row go the same way.
 template <int P, bool TAIL>
 __device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[P][kPiece], bool layer, int width, float eps, Team &team)
 {
@@ -260,15 +261,15 @@ __device__ __forceinline__ void normalise(const Row<P, TAIL> &r, float (&v)[P][k
     if (!(q >= 0x1p-80f && q <= 0x1p100f)) {
         const int top = largest(r, v, team);
         if (top < 0x7f800000) { // (an infinity or NaN spoils its row either way)
-            // the largest magnitude to about 1: factors 2^up, two of them where one is no normal number
-            const int up = 127 - max(top >> 23, 1);
+            // the largest magnitude to about 1, or (eps) to that at most: factors 2^up, two of them where one is no normal number
+            const int up = 127 - max(top >> 23, eps > 0.0f ? 127 : 1);
             const float a = __uint_as_float((uint32_t)(127 + up / 2) << 23), b = __uint_as_float((uint32_t)(127 + (up - up / 2)) << 23);
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) v[p][i] = v[p][i] * a * b;
             s = spread_of(r, v, layer, width, team);
-            q = s.square + eps * a * b * a * b;
+            q = s.square + (eps > 0.0f ? fmaxf(eps * a * b * a * b, 0x1p-126f) : 0.0f);
         }
     }
     const float by = 1.0f / sqrtf(q);
