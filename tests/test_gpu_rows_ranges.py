@@ -47,3 +47,73 @@ def test_large_rows_with_an_eps(layer):
             h[t, :width] = h[t, :width] * 2.0 ** e
         m.check(h)
         m.check(rows(5, width, torch.bfloat16, 2), h)
+
+
+def gates(dtype):
+    """every 16-bit number from 2^-20 to 256, of both signs, and some beyond"""
+    t = DTYPES[dtype][1]
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(t)
+    bits = bits[(bits.abs() >= 2.0 ** -20) & (bits.abs() <= 256)]
+    more = torch.tensor([0.0, -0.0, 1e3, -1e3, 6e4, -6e4] + ([1e20, -1e20, 3e38, -3e38] if dtype == "bf16" else []), dtype=torch.float32).to(t)
+    return torch.cat([bits, more])
+
+
+@pytest.mark.parametrize("kind", [slora.ACT_SILU, slora.ACT_GELU])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [0, 20, 60, 100, 120, 126, -20])
+def test_gates_of_every_size(dtype, kind, size):
+    """x act(g) to 12 half-steps of fp32 (E each) before it is rounded, however small act(g) is; E are counted as: exp2(r) 2 and r's own roundings (of |r| <= 1, four at most,
+    2^-25 each times ln 2) 1.4, both once more halved in 1 + z; that sum 1, its reciprocal 2, three products 3: 3.4 + 1.7 + 1 + 2 + 3 < 12.
+    x 2^n below 2^-126 is off by 2^-150 at most, times at most |g| < 2^8 where the result is not 0.  Products of 0 and results beyond the type's range are left out."""
+    lib, t = DTYPES[dtype]
+    if dtype == "f16" and abs(size) > 20:
+        pytest.skip("binary16 has no such x")
+    g = gates(dtype)
+    width = -(-len(g) // 8) * 8
+    gate = torch.zeros((2, width), dtype=t)
+    gate[:, :len(g)] = g
+    rng = np.random.default_rng(abs(size))
+    scale = min(size, 14) if dtype == "f16" else size
+    x = (torch.from_numpy(rng.uniform(1, 2, (2, width)) * rng.choice([-1, 1], (2, width))) * 2.0 ** scale).to(t)
+    d_gate, d_x, y = gate.cuda(), x.cuda(), torch.empty((2, width), dtype=t, device="cuda")
+    slora.w8_quantize(2, width, lib, kind, d_x.data_ptr(), width, d_gate.data_ptr(), width, y.data_ptr(), width)
+    torch.cuda.synchronize()
+    with np.errstate(over="ignore", invalid="ignore"):
+        gd = gate.double().numpy()
+        u = gd if kind == slora.ACT_SILU else 2 * np.sqrt(2 / np.pi) * (gd + 0.044715 * gd ** 3)
+        ref = gd / (1 + np.exp(-u)) * x.double().numpy()
+    keep = np.isfinite(ref) & (np.abs(ref) < torch.finfo(t).max * (1 - 2.0 ** -8))
+    bound = 12 * du.E * np.abs(ref) + 2.0 ** -142
+    du.within(y.reshape(-1)[torch.from_numpy(np.flatnonzero(keep)).cuda()], ref[keep], bound[keep])
+
+
+@pytest.mark.parametrize("kind", [slora.ACT_SILU, slora.ACT_GELU])
+def test_codes_of_gated_rows_are_as_close_as_fp32_allows(kind):
+    """codes of rows whose gates are all -1, -5, -20, ... times x: x act(g) to 12 half-steps of fp32, so that only a code that lies so near a tie may be another"""
+    width, T = 4096, 8
+    x = rows(T, width, torch.float16, 4)
+    gate = torch.empty_like(x)
+    for t, g in enumerate([-0.01, -0.3, -1.0, -3.0, -4.5, 5.0, 20.0, 300.0]):
+        gate[t] = g
+    codes, scales = torch.empty((T, width), dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    slora.w8_quantize(T, width, slora.F16, kind, x.data_ptr(), width, gate.data_ptr(), width, codes=codes.data_ptr(), codes_stride=width, scales=scales.data_ptr())
+    torch.cuda.synchronize()
+    g, v = gate.double().cpu().numpy(), x[:, :width].double().cpu().numpy()
+    ref = v * g / (1 + np.exp(-(g if kind == slora.ACT_SILU else 2 * np.sqrt(2 / np.pi) * (g + 0.044715 * g ** 3))))
+    du.codes_within(codes, scales, ref, 12 * du.E * np.abs(ref))
+
+
+@pytest.mark.parametrize("kind", [slora.ACT_SILU, slora.ACT_GELU])
+@pytest.mark.parametrize("width", [1, 13, 515, 1003, 5003, 13007])
+def test_what_is_behind_a_row_changes_nothing_in_it(width, kind):
+    T = 6
+    x, gate, out = rows(T, width, torch.bfloat16, 1, pad=8), rows(T, width, torch.bfloat16, 2, pad=8, size=2.0), []
+    for behind in (0.0, float("nan"), -1e30):
+        x[:, width:], gate[:, width:] = behind, behind
+        y, codes, scales = torch.empty_like(x), torch.empty((T, -(-width // 16) * 16), dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+        slora.w8_quantize(T, width, slora.BF16, kind, x.data_ptr(), x.stride(0), gate.data_ptr(), gate.stride(0), y.data_ptr(), y.stride(0), codes.data_ptr(), codes.stride(0),
+                          scales.data_ptr())
+        torch.cuda.synchronize()
+        out.append((y[:, :width], codes[:, :width], scales))
+    for other in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(out[0], other))
