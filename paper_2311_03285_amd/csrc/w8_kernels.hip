@@ -54,9 +54,19 @@ __global__ __launch_bounds__(256) void w8_pack_kernel(const int8_t *__restrict__
 __device__ __forceinline__ i32x4 mfma16(const i32x4 &a, const i32x4 &b, const i32x4 &c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ i32x16 mfma32(const i32x4 &a, const i32x4 &b, const i32x16 &c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 
-// Y: 0 fp32, else 1 + the 16-bit type.  The sum, exact so far, is rounded to fp32 and multiplied by both scales there; the product of the scales
-// alone could leave the range that the three have.
-__device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale) { return (float)sum * x_scale * w_scale; }
+// The sum, exact so far, is rounded to fp32 and multiplied by both scales there; the product of the scales alone could leave the range that the three have.  So could the
+// sum, up to 2^31, times a scale of x above 2^96 (a row of bfloat16 has up to 2^121): of that, 2^32 wait until the end.  What is left is above 2^64, so that no weight's
+// scale makes a subnormal number of it, and results are the same to the bit.
+struct XScale {
+    float now, rest;
+    __device__ __forceinline__ explicit XScale(float s)
+    {
+        const bool far = fabsf(s) > 0x1p96f;
+        now = far ? s * 0x1p-32f : s;
+        rest = far ? 0x1p32f : 1.0f;
+    }
+};
+// Y: 0 fp32, else 1 + the 16-bit type
 template <int Y>
 __device__ __forceinline__ void store_y(void *y, int64_t at, float v)
 {
@@ -144,7 +154,8 @@ __global__ __launch_bounds__(kFewWaves *kWave) void w8_few_kernel(W8Args a)
         int total = 0;
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k) total += part[k][r / 16][t % 4][t / 4 * 16 + r % 16];
-        store_y<Y>(m.y, (int64_t)t * m.y_stride + o, scaled(total, m.x_scales[t], m.scales[o]));
+        const XScale by(m.x_scales[t]);
+        store_y<Y>(m.y, (int64_t)t * m.y_stride + o, (float)total * by.now * m.scales[o] * by.rest);
     }
 }
 
@@ -335,7 +346,8 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
         const int tw = t0 + (wt * MT + j) * 32;
-        const float x_scale = m.x_scales[min(tw + n, a.T - 1)];
+        const XScale by(m.x_scales[min(tw + n, a.T - 1)]);
+        const bool far = __builtin_amdgcn_ballot_w64(by.rest != 1.0f) != 0;
 #pragma unroll
         for (int i = 0; i < MO; ++i)
 #pragma unroll
@@ -343,7 +355,11 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
                 const f32x4 w_scale = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = scaled(sum[i][j][4 * b + e], x_scale, w_scale[e]);
+                for (int e = 0; e < 4; ++e) v[e] = (float)sum[i][j][4 * b + e] * by.now * w_scale[e];
+                if (far) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] *= by.rest;
+                }
                 char *const to = stage + n * kPitch + (i * 32 + 8 * b + 4 * h) * sizeof(Out);
                 if constexpr (Y == 0)
                     *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
