@@ -7,6 +7,38 @@
 
 using namespace slora;
 
+namespace slora {
+
+int64_t w8_parts(const W8Args &a, int each)
+{
+    int64_t n = 0;
+    for (int32_t k = 0; k < a.n; ++k) n += ((int64_t)a.m[k].outputs + each - 1) / each;
+    return n;
+}
+
+// The shape whose workgroups, of which compute units take rounds, are done first, by what a stage of one takes (measured with one and with
+// several rounds, where clocks are lower).  The larger the shape, the less is read for each product; the smaller, the more compute units have one.
+// us: 256 x 256 against the next ones, 8192 tokens of 8192 x 8192 453 / 500 / 519, two of 20480 of 5120, 2048 tokens 387 / 418 / 441; 256 x 192 / 256 x 256, 5120 of
+// 20480, 2048 tokens 197 / 211; 256 x 128 / 128 x 128, three of 4096 of 4096, 512 tokens 34 / 37; 128 x 192 / 128 x 128, three of 5003 of 3083, 333 tokens 33 / 42;
+// 128 x 128 / 256 x 128, 4096 of 4096, 1024 tokens 25 / 30; 64 x 128 / 128 x 128, 512 tokens 17 / 22; 64 x 64 / 64 x 128, 200 tokens 13 / 15; 64 x 32 / 64 x 64, three,
+// 24 tokens 14.5 / 15.0; 32 x 32 / 64 x 32, 64 tokens 8.8 / 11.9.  Teams: 64 x 64 with two 12.6, with one 17.8 (4096 of 4096, 64 tokens).
+int w8_shape(const W8Args &a)
+{
+    int best = 0;
+    float least = 0.0f;
+    for (int i = 0; i < (int)(sizeof(kW8Shapes) / sizeof(kW8Shapes[0])); ++i) {
+        const int64_t groups = w8_parts(a, kW8Shapes[i].outputs) * (((int64_t)a.T + kW8Shapes[i].tokens - 1) / kW8Shapes[i].tokens);
+        const float us = (float)w8_rounds(groups) * kW8Shapes[i].us;
+        if (i == 0 || (us < least && groups * kW8Shapes[i].threads <= kMostThreads)) {
+            best = i;
+            least = us;
+        }
+    }
+    return best;
+}
+
+} // namespace slora
+
 namespace {
 
 int32_t check_shape(int32_t outputs, int32_t inputs)

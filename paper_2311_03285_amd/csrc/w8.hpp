@@ -34,6 +34,21 @@ struct W8Args {
     int32_t n, T;
 };
 
+// How calls of more than 16 tokens are cut into workgroups
+struct W8Shape {
+    int outputs, tokens, threads;
+    float us; // of a stage of 128 inputs
+};
+constexpr W8Shape kW8Shapes[] = {{256, 256, 512, 1.7f}, {256, 192, 512, 1.27f}, {256, 128, 512, 0.95f}, {128, 192, 512, 0.74f}, {128, 128, 256, 0.56f},
+                                 {64, 128, 512, 0.42f}, {64, 64, 512, 0.3f},    {64, 32, 256, 0.2f},    {32, 32, 256, 0.18f}};
+constexpr int64_t kComputeUnits = 256;
+constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1; // of a grid
+inline int64_t w8_rounds(int64_t groups) { return (groups + kComputeUnits - 1) / kComputeUnits; }
+
+// w8.cpp
+int64_t w8_parts(const W8Args &a, int each); // how many of `each` outputs there are
+int w8_shape(const W8Args &a);               // of kW8Shapes
+
 // w8_kernels.hip
 int32_t launch_w8_pack(const slora_w8 *w, const int8_t *codes, const float *scales, void *packed, void *stream);
 // y: 0 fp32, else 1 + the 16-bit type

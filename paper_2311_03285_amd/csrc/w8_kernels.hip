@@ -398,8 +398,6 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
     }
 }
 
-constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1; // of a grid
-
 // workgroups of `each` outputs, `blocks` of tokens; returns how many, which may be too many for a grid
 int64_t share_out(W8Args &a, int each, int64_t blocks)
 {
@@ -420,12 +418,13 @@ int32_t launch_few(W8Args &a, void *stream)
     return check_launch("w8_few");
 }
 
-template <int TEAMS, int WO, int WT, int MO, int MT, bool ONCE, int Y>
+template <int SHAPE, int TEAMS, int WO, int WT, int MO, int MT, bool ONCE, int Y>
 int32_t launch_tile(W8Args &a, void *stream)
 {
     typedef Tile<TEAMS, WO, WT, MO, MT> Shape;
     constexpr int kLds = Shape::lds(Y == 0 ? 4 : 2);
     static_assert(kLds <= 160 * 1024, "LDS");
+    static_assert(kW8Shapes[SHAPE].outputs == Shape::BO && kW8Shapes[SHAPE].tokens == Shape::BT && kW8Shapes[SHAPE].threads == Shape::kThreads, "the shape that w8_shape has chosen");
     const int64_t groups = share_out(a, Shape::BO, ((int64_t)a.T + Shape::BT - 1) / Shape::BT);
     if (groups * Shape::kThreads > kMostThreads) return fail(SLORA_ERANGE, "T=%d tokens of so many outputs are too many for one call", a.T);
     if (kLds > 65536) {
@@ -436,68 +435,36 @@ int32_t launch_tile(W8Args &a, void *stream)
     return check_launch("w8_tile");
 }
 
-constexpr int64_t kComputeUnits = 256;
-
-// How many of `each` outputs there are.
-int64_t parts(const W8Args &a, int each)
-{
-    int64_t n = 0;
-    for (int32_t k = 0; k < a.n; ++k) n += ((int64_t)a.m[k].outputs + each - 1) / each;
-    return n;
-}
-int64_t rounds(int64_t groups) { return (groups + kComputeUnits - 1) / kComputeUnits; }
-
 // Up to 16 tokens: one tile of outputs a workgroup or two, by the bytes that the compute unit with most workgroups reads.  us with one / two: 16 tokens, two of 20480 of
 // 5120 52 / 39, 5120 of 20480 37 / 28, 4096 of 4096 5.8 / 6.7; 8 tokens, three of 4096 of 4096 10.6 / 11.3.
 template <int Y>
 int32_t few(W8Args &a, void *stream)
 {
-    const int64_t tiles = parts(a, kW8Rows);
-    if (rounds(tiles) * (16 + a.T) <= rounds((tiles + 1) / 2) * (32 + a.T) && tiles * kFewWaves * kWave <= kMostThreads) return launch_few<1, Y>(a, stream);
+    const int64_t tiles = w8_parts(a, kW8Rows);
+    if (w8_rounds(tiles) * (16 + a.T) <= w8_rounds((tiles + 1) / 2) * (32 + a.T) && tiles * kFewWaves * kWave <= kMostThreads) return launch_few<1, Y>(a, stream);
     return launch_few<2, Y>(a, stream);
 }
 
-// More tokens: the shape whose workgroups, of which compute units take rounds, are done first, by what a stage of one takes (measured with one and with
-// several rounds, where clocks are lower).  The larger the shape, the less is read for each product; the smaller, the more compute units have one.
-// us: 256 x 256 against the next ones, 8192 tokens of 8192 x 8192 453 / 500 / 519, two of 20480 of 5120, 2048 tokens 387 / 418 / 441; 256 x 192 / 256 x 256, 5120 of
-// 20480, 2048 tokens 197 / 211; 256 x 128 / 128 x 128, three of 4096 of 4096, 512 tokens 34 / 37; 128 x 192 / 128 x 128, three of 5003 of 3083, 333 tokens 33 / 42;
-// 128 x 128 / 256 x 128, 4096 of 4096, 1024 tokens 25 / 30; 64 x 128 / 128 x 128, 512 tokens 17 / 22; 64 x 64 / 64 x 128, 200 tokens 13 / 15; 64 x 32 / 64 x 64, three,
-// 24 tokens 14.5 / 15.0; 32 x 32 / 64 x 32, 64 tokens 8.8 / 11.9.  Teams: 64 x 64 with two 12.6, with one 17.8 (4096 of 4096, 64 tokens).
 template <int Y>
 int32_t many(W8Args &a, void *stream)
 {
-    constexpr struct {
-        int outputs, tokens, threads;
-        float us;
-    } kShapes[] = {{256, 256, 512, 1.7f}, {256, 192, 512, 1.27f}, {256, 128, 512, 0.95f}, {128, 192, 512, 0.74f}, {128, 128, 256, 0.56f},
-                   {64, 128, 512, 0.42f}, {64, 64, 512, 0.3f},    {64, 32, 256, 0.2f},    {32, 32, 256, 0.18f}};
-    int best = 0;
-    float least = 0.0f;
-    for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
-        const int64_t groups = parts(a, kShapes[i].outputs) * (((int64_t)a.T + kShapes[i].tokens - 1) / kShapes[i].tokens);
-        const float us = (float)rounds(groups) * kShapes[i].us;
-        if (i == 0 || (us < least && groups * kShapes[i].threads <= kMostThreads)) {
-            best = i;
-            least = us;
-        }
-    }
     // The weights of large calls are loaded once each, but by the largest shapes, whose tiles of tokens share them.  us with / without, inputs that are not in any cache: two of 20480
     // of 5120, 32 tokens 38.2 / 42.3, 100 tokens 45.5 / 48.1; four of 4096 of 4096, 128 tokens 19.6 / 21.7; two of 20480 of 5120, 2048 tokens (256 x 256) 395 / 381.
     // Of 50 MB that are in the memory-side cache: three of 4096 of 4096, 24 tokens behind a norm 19.2 / 17.5.
     int64_t bytes = 0;
     for (int32_t k = 0; k < a.n; ++k) bytes += (int64_t)a.m[k].tiles * a.m[k].chunks * kW8Block;
     auto by_once = [&](auto launch) { return bytes >= kOnceBytes ? launch(std::true_type{}) : launch(std::false_type{}); };
-    switch (best) {
-    case 0: return launch_tile<1, 2, 4, 4, 2, false, Y>(a, stream);
-    case 1: return launch_tile<1, 4, 2, 2, 3, false, Y>(a, stream);
-    case 2: return by_once([&](auto once) { return launch_tile<1, 4, 2, 2, 2, once.value, Y>(a, stream); });
-    case 3: return by_once([&](auto once) { return launch_tile<1, 4, 2, 1, 3, once.value, Y>(a, stream); });
-    case 4: return by_once([&](auto once) { return launch_tile<1, 2, 2, 2, 2, once.value, Y>(a, stream); });
-    case 5: return by_once([&](auto once) { return launch_tile<2, 2, 2, 1, 2, once.value, Y>(a, stream); });
-    case 6: return by_once([&](auto once) { return launch_tile<2, 2, 2, 1, 1, once.value, Y>(a, stream); });
-    case 7: return by_once([&](auto once) { return launch_tile<2, 2, 1, 1, 1, once.value, Y>(a, stream); });
+    switch (w8_shape(a)) {
+    case 0: return launch_tile<0, 1, 2, 4, 4, 2, false, Y>(a, stream);
+    case 1: return launch_tile<1, 1, 4, 2, 2, 3, false, Y>(a, stream);
+    case 2: return by_once([&](auto once) { return launch_tile<2, 1, 4, 2, 2, 2, once.value, Y>(a, stream); });
+    case 3: return by_once([&](auto once) { return launch_tile<3, 1, 4, 2, 1, 3, once.value, Y>(a, stream); });
+    case 4: return by_once([&](auto once) { return launch_tile<4, 1, 2, 2, 2, 2, once.value, Y>(a, stream); });
+    case 5: return by_once([&](auto once) { return launch_tile<5, 2, 2, 2, 1, 2, once.value, Y>(a, stream); });
+    case 6: return by_once([&](auto once) { return launch_tile<6, 2, 2, 2, 1, 1, once.value, Y>(a, stream); });
+    case 7: return by_once([&](auto once) { return launch_tile<7, 2, 2, 1, 1, 1, once.value, Y>(a, stream); });
     }
-    return by_once([&](auto once) { return launch_tile<4, 1, 1, 1, 1, once.value, Y>(a, stream); });
+    return by_once([&](auto once) { return launch_tile<8, 4, 1, 1, 1, 1, once.value, Y>(a, stream); });
 }
 
 } // namespace
