@@ -37,6 +37,19 @@ int w8_shape(const W8Args &a)
     return best;
 }
 
+// Weights that are large, and that each are read by one workgroup or by several that run at the same time; with more rounds of workgroups the next tile of tokens finds in the memory-side cache
+// what keeps its place.  us with / without a place, weights that are in no cache before: one tile of tokens, two of 20480 of 5120, 32 tokens 43.1 / 39.6, 100 tokens 49.3 / 46.9, four of 4096 of
+// 4096, 128 tokens 23.6 / 20.4; one round, four of 4096 of 4096, 512 tokens 41.2 / 40.1, 8192 of 8192, 200 tokens 29.9 / 28.6, but 5120 of 20480, 300 tokens 58.5 / 62.8; more rounds, two of 20480 of
+// 5120, 200 tokens 78 / 92, 900 tokens 227 / 273.  The largest two shapes read them at the same speed either way.
+// Smaller weights gain less or lose, if they are still there: three of 4096 of 4096, 24 tokens, 14.2 / 13.5 from memory, 11.6 / 13.0 where all the weights that take turns are 200 MB.
+bool w8_once(const W8Args &a, const W8Shape &s)
+{
+    int64_t bytes = 0;
+    for (int32_t k = 0; k < a.n; ++k) bytes += (int64_t)a.m[k].tiles * a.m[k].chunks * kW8Block;
+    const int64_t tiles = ((int64_t)a.T + s.tokens - 1) / s.tokens;
+    return bytes >= kOnceWeights && (tiles == 1 || w8_rounds(w8_parts(a, s.outputs) * tiles) == 1);
+}
+
 } // namespace slora
 
 namespace {

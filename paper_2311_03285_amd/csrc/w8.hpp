@@ -42,12 +42,14 @@ struct W8Shape {
 constexpr W8Shape kW8Shapes[] = {{256, 256, 512, 1.7f}, {256, 192, 512, 1.27f}, {256, 128, 512, 0.95f}, {128, 192, 512, 0.74f}, {128, 128, 256, 0.56f},
                                  {64, 128, 512, 0.42f}, {64, 64, 512, 0.3f},    {64, 32, 256, 0.2f},    {32, 32, 256, 0.18f}};
 constexpr int64_t kComputeUnits = 256;
+constexpr int64_t kOnceWeights = 64 << 20; // bytes
 constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1; // of a grid
 inline int64_t w8_rounds(int64_t groups) { return (groups + kComputeUnits - 1) / kComputeUnits; }
 
 // w8.cpp
 int64_t w8_parts(const W8Args &a, int each); // how many of `each` outputs there are
 int w8_shape(const W8Args &a);               // of kW8Shapes
+bool w8_once(const W8Args &a, const W8Shape &s); // whether its weights are loaded without a place in the caches
 
 // w8_kernels.hip
 int32_t launch_w8_pack(const slora_w8 *w, const int8_t *codes, const float *scales, void *packed, void *stream);

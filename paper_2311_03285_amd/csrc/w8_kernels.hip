@@ -448,13 +448,9 @@ int32_t few(W8Args &a, void *stream)
 template <int Y>
 int32_t many(W8Args &a, void *stream)
 {
-    // The weights of large calls are loaded once each, but by the largest shapes, whose tiles of tokens share them.  us with / without, inputs that are not in any cache: two of 20480
-    // of 5120, 32 tokens 38.2 / 42.3, 100 tokens 45.5 / 48.1; four of 4096 of 4096, 128 tokens 19.6 / 21.7; two of 20480 of 5120, 2048 tokens (256 x 256) 395 / 381.
-    // Of 50 MB that are in the memory-side cache: three of 4096 of 4096, 24 tokens behind a norm 19.2 / 17.5.
-    int64_t bytes = 0;
-    for (int32_t k = 0; k < a.n; ++k) bytes += (int64_t)a.m[k].tiles * a.m[k].chunks * kW8Block;
-    auto by_once = [&](auto launch) { return bytes >= kOnceBytes ? launch(std::true_type{}) : launch(std::false_type{}); };
-    switch (w8_shape(a)) {
+    const int shape = w8_shape(a);
+    auto by_once = [&](auto launch) { return w8_once(a, kW8Shapes[shape]) ? launch(std::true_type{}) : launch(std::false_type{}); };
+    switch (shape) {
     case 0: return launch_tile<0, 1, 2, 4, 4, 2, false, Y>(a, stream);
     case 1: return launch_tile<1, 1, 4, 2, 2, 3, false, Y>(a, stream);
     case 2: return by_once([&](auto once) { return launch_tile<2, 1, 4, 2, 2, 2, once.value, Y>(a, stream); });
