@@ -348,25 +348,31 @@ __global__ __launch_bounds__(TEAMS *WO *WT *kWave, tile_occupancy(MO *MT)) void 
         const int tw = t0 + (wt * MT + j) * 32;
         const XScale by(m.x_scales[min(tw + n, a.T - 1)]);
         const bool far = __builtin_amdgcn_ballot_w64(by.rest != 1.0f) != 0;
+        auto put_y = [&](auto far) {
 #pragma unroll
-        for (int i = 0; i < MO; ++i)
+            for (int i = 0; i < MO; ++i)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const f32x4 w_scale = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
-                float v[4];
+                for (int b = 0; b < 4; ++b) {
+                    const f32x4 w_scale = *reinterpret_cast<const f32x4 *>(m.scales + min(ow + i * 32 + 8 * b + 4 * h, m.tiles * kW8Rows - 4));
+                    float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (float)sum[i][j][4 * b + e] * by.now * w_scale[e];
-                if (far) {
+                    for (int e = 0; e < 4; ++e) v[e] = (float)sum[i][j][4 * b + e] * by.now * w_scale[e];
+                    if constexpr (far.value) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] *= by.rest;
+                        for (int e = 0; e < 4; ++e) v[e] *= by.rest;
+                    }
+                    char *const to = stage + n * kPitch + (i * 32 + 8 * b + 4 * h) * sizeof(Out);
+                    if constexpr (Y == 0)
+                        *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
+                    else
+                        *reinterpret_cast<u32x2 *>(to) = u32x2{(uint32_t)narrow<Y - 1>(v[0]) | (uint32_t)narrow<Y - 1>(v[1]) << 16,
+                                                               (uint32_t)narrow<Y - 1>(v[2]) | (uint32_t)narrow<Y - 1>(v[3]) << 16};
                 }
-                char *const to = stage + n * kPitch + (i * 32 + 8 * b + 4 * h) * sizeof(Out);
-                if constexpr (Y == 0)
-                    *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
-                else
-                    *reinterpret_cast<u32x2 *>(to) = u32x2{(uint32_t)narrow<Y - 1>(v[0]) | (uint32_t)narrow<Y - 1>(v[1]) << 16,
-                                                           (uint32_t)narrow<Y - 1>(v[2]) | (uint32_t)narrow<Y - 1>(v[3]) << 16};
-            }
+        };
+        if (far)
+            put_y(std::true_type{});
+        else
+            put_y(std::false_type{});
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
