@@ -10,9 +10,6 @@ namespace slora {
 namespace {
 
 constexpr int kWave = 64;
-// Inputs of a call that are this large are not in the caches from whatever wrote or read them last - the memory-side cache holds 256 MiB - and are loaded without a place there.
-// Smaller ones may be: rows from the kernel that wrote them, weights of a few layers from the step before.
-constexpr int64_t kOnceBytes = 64 << 20;
 
 template <int DT>
 __device__ __forceinline__ float widen(uint16_t b)

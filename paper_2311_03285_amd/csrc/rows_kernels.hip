@@ -55,8 +55,12 @@ __device__ __forceinline__ void widen8(const u32x4 &raw, float (&v)[kPiece])
     for (int i = 0; i < kPiece; ++i) v[i] = widen<DT>((uint16_t)(raw[i / 2] >> (16 * (i % 2))));
 }
 
-// ONCE: rows are loaded without a place in the caches (vectors that all rows read always with one).  us with / without, of rows that are in none: gated 3001 rows of 13007 40 / 44, 8192 rows of
-// 4096 through a norm 44.5 / 48.7; of rows that are in the memory-side cache: 4096 of 5120 to 8 bits 13.6 / 12.1, norms of 777 of 5003 18.4 / 15.1.
+// ONCE: rows are loaded without a place in the caches (vectors that all rows read always with one): those of calls with this many bytes of them or more.  No bound of a cache: the
+// memory-side one holds 256 MiB and may have rows of this size from the kernel that wrote them; by what was measured.  us with / without a place, rows that a product has just written:
+// gated products of 2048 rows of 20480 (160 MiB) 54.8 / 53.7, 3000 (234) 80.6 / 73.9, 1024 (80) 28.9 / 25.6, a norm of 8192 rows of 5120 (160) 63.0 / 57.9, of 4096 (80) 32.3 / 35.2;
+// rows that are in no cache: 4096 of 5120 (40) 13.5 / 13.6, 2048 of 20480 (80) 29.6 / 30.3, norms of 8192 of 4096 48.7 / 44.5; rows read again from the memory-side cache: 4096 of
+// 5120 12.1 / 12.6, 2048 of 20480 25.0 / 30.4.
+constexpr int64_t kOnceBytes = 64 << 20;
 template <bool ONCE, typename T>
 __device__ __forceinline__ T load_piece(const T *from)
 {
