@@ -480,13 +480,19 @@ struct Gate {
         power = __builtin_amdgcn_exp2f(r);
         whole = (int)n;
     }
+    __device__ __forceinline__ float z() const { return __builtin_ldexpf(power, whole); }
     static __device__ __forceinline__ float quotient(float z) { return __builtin_amdgcn_rcpf(1.0f + z); }
-    // Gates from -kSmall to kSmall: z < 2^116 and its quotient are in range.
-    static constexpr float kSmall = ACT == SLORA_ACT_SILU ? 80.0f : 9.0f;
+    // Gates from -kSmall to kSmall: z < 2^96 and its quotient are in range.  silu needs no whole part there: what t = -g log2 e is off by as a number is -g - t ln 2, one fused step, by
+    // which z is put right.  (ln 2 is off by 0.05 half-steps, of up to 40: 1.9; the exponential 2, this step 1, 1 + z 1, its reciprocal 2, two products.)
+    static constexpr float kSmall = ACT == SLORA_ACT_SILU ? 40.0f : 9.0f;
     static __device__ __forceinline__ float small(float x, float g)
     {
-        const Gate e(g);
-        return x * (g * quotient(__builtin_ldexpf(e.power, e.whole)));
+        if constexpr (ACT == SLORA_ACT_SILU) {
+            const float t = g * -kAHigh, power = __builtin_amdgcn_exp2f(t);
+            return x * (g * quotient(__builtin_fmaf(power, __builtin_fmaf(t, -0.693147180559945309417f, -g), power)));
+        } else {
+            return x * (g * quotient(Gate(g).z()));
+        }
     }
     // All gates: z of -|g|, and for negative g 1 / (1 + 1 / z) = z / (1 + z), whose 2^n goes to x - there is a result wherever the product of all has one, though act(g) alone
     // may be below fp32's range.
@@ -494,12 +500,12 @@ struct Gate {
     {
         const Gate e(fminf(fabsf(g), 256.0f)); // (z is 0 from there on; NaN comes back with g)
         const bool negative = g < 0.0f;
-        return __builtin_ldexpf(x, negative ? e.whole : 0) * (g * (quotient(__builtin_ldexpf(e.power, e.whole)) * (negative ? e.power : 1.0f)));
+        return __builtin_ldexpf(x, negative ? e.whole : 0) * (g * (quotient(e.z()) * (negative ? e.power : 1.0f)));
     }
 };
 
 // A piece whose gates are all small in all of the wavefront goes without the steps for the others (which round elsewhere: not by what is behind the row, so that a piece
-// that is not whole takes them always).  us of 3001 rows of 13007, silu / gelu, inputs that are in no cache: 46.9 / 48.1, all pieces with these steps 54 / 56; with u log2 e rounded 46.2 / 45.7.
+// that is not whole takes them always).
 template <int ACT, int DT>
 __device__ __forceinline__ void gate_piece(float (&v)[kPiece], const u32x4 &gate, bool whole)
 {
@@ -521,9 +527,12 @@ __device__ __forceinline__ void gate_piece(float (&v)[kPiece], const u32x4 &gate
 }
 
 // Rows in 8 bits, or the gated product, as norms are taken: one row for the workgroup, or one for each of its wavefronts.
-// Bound: HBM (3001 gated rows of 13007, 234 MB: 40 us = 5.9 TB/s; 4096 rows of 5120 to 8 bits, 63 MB: 12.1 us = 5.2 TB/s).
-template <int DT, int P, bool TAIL, bool ONCE>
-__global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, int waves)
+// Bound, plain rows: HBM (4096 of 5120 to 8 bits that are in no cache, 63 MB: 15.1 us = 4.2 TB/s; in the memory-side cache 12.1).  Gated ones: HBM beside the vector units - us to 8 bits with
+// no gate / silu / gelu, 2048 rows of 20480 23.6 / 40.2 / 49.0, 3001 of 13008 23.1 / 39.5 / 47.1, of 13007 24.7 / 43.9 / 51.6 (the pieces of the last wavefront, above), and with u log2 e rounded as a
+// number, which leaves fp32's accuracy, silu 40.7 / 38.6 / 40.9.  A kernel for each function: all three in one take more registers and 25.9 us without a gate, 41.2 with silu (3001 of 13008).
+// With six wavefronts a SIMD asked for, rows of ten wavefronts run two to a compute unit: 2048 of 20480, silu 43.1 without, 40.2 with.
+template <int DT, int ACT, int P, bool TAIL, bool ONCE>
+__global__ __launch_bounds__(kRowThreads, P == 8 ? 4 : 6) void quantize_kernel(QuantizeArgs a, int waves)
 {
     __shared__ uint32_t slots[1][kRowThreads / kWave];
     const int wave = wave_number();
@@ -533,24 +542,13 @@ __global__ __launch_bounds__(kRowThreads) void quantize_kernel(QuantizeArgs a, i
     Team team{slots, waves, wave};
     u32x4 raw[P], gate[P];
     load16<ONCE>(r, a.x + t * a.x_stride, raw);
-    if (a.gate) load16<ONCE>(r, a.gate + t * a.gate_stride, gate);
+    if constexpr (ACT != SLORA_ACT_NONE) load16<ONCE>(r, a.gate + t * a.gate_stride, gate);
     float v[P][kPiece];
-    // Which function it is is asked once, but for rows of eight pieces, which have no registers for more than one piece under way.  us of 2048 rows of 20480, silu / gelu, asked
-    // once 46.5 / 49.3, for each piece 49.4 / 55.4.
-    constexpr int kStep = P == 8 ? 1 : P;
     const Row<P, TAIL> now = again(r);
 #pragma unroll
-    for (int first = 0; first < P; first += kStep) {
-#pragma unroll
-        for (int p = first; p < first + kStep; ++p) widen8<DT>(raw[p], v[p]);
-        if (a.act == SLORA_ACT_SILU) {
-#pragma unroll
-            for (int p = first; p < first + kStep; ++p) gate_piece<SLORA_ACT_SILU, DT>(v[p], gate[p], now.whole(p));
-        }
-        if (a.act == SLORA_ACT_GELU) {
-#pragma unroll
-            for (int p = first; p < first + kStep; ++p) gate_piece<SLORA_ACT_GELU, DT>(v[p], gate[p], now.whole(p));
-        }
+    for (int p = 0; p < P; ++p) {
+        widen8<DT>(raw[p], v[p]);
+        if constexpr (ACT != SLORA_ACT_NONE) gate_piece<ACT, DT>(v[p], gate[p], now.whole(p));
     }
     if (a.out.x) store16<DT>(r, a.out.x + t * a.out.x_stride, v);
     if (a.out.codes) store_codes(r, a.out, t, v, team);
@@ -615,15 +613,24 @@ int32_t launch_norm(const NormArgs &a, int32_t dtype, bool h32, void *stream)
 int32_t launch_quantize(const QuantizeArgs &a, int32_t dtype, void *stream)
 {
     const int64_t bytes = (int64_t)a.T * a.width * (a.gate ? 4 : 2);
+    auto by_act = [&](auto f) {
+        switch (a.act) {
+        case SLORA_ACT_SILU: return f(std::integral_constant<int, SLORA_ACT_SILU>{});
+        case SLORA_ACT_GELU: return f(std::integral_constant<int, SLORA_ACT_GELU>{});
+        }
+        return f(std::integral_constant<int, SLORA_ACT_NONE>{});
+    };
     return by_width<8>(a.width, [&](auto p, int waves) {
         return by_flag(a.width % kPiece != 0, [&](auto tail) {
             return by_flag(bytes >= kOnceBytes, [&](auto once) {
-                const Grid g(a.T, waves);
-                if (dtype == SLORA_F16)
-                    hipLaunchKernelGGL((quantize_kernel<SLORA_F16, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-                else
-                    hipLaunchKernelGGL((quantize_kernel<SLORA_BF16, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
-                return check_launch("quantize");
+                return by_act([&](auto act) {
+                    const Grid g(a.T, waves);
+                    if (dtype == SLORA_F16)
+                        hipLaunchKernelGGL((quantize_kernel<SLORA_F16, act.value, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                    else
+                        hipLaunchKernelGGL((quantize_kernel<SLORA_BF16, act.value, p.value, tail.value, once.value>), g.blocks, g.threads, 0, (hipStream_t)stream, a, waves);
+                    return check_launch("quantize");
+                });
             });
         });
     });
