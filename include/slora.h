@@ -545,8 +545,8 @@ int32_t slora_norm_destroy(slora_norm *norm);
  * h; h_out: h', rounded once; NULL: not wanted.
  * block: b, of `dtype`; NULL: h' = h (gate has to be NULL).  gate: of `dtype`, a row for each token, or with gate_stride 0 one for all; NULL: 1.
  * x: of `dtype`; codes, scales: x in 8 bits, of the fp32 values that x is rounded from; NULL (scales with codes): not wanted.
- * Norms are of h' before it is rounded; sums are fp32.  16-byte aligned, strides multiples of 8 (codes: of 16) and at
- * least `width`; nothing behind a row's `width` elements is written, and what is read there, up to the next 16 bytes' end, may be anything.  h_out may be h, x may be block, of equal strides; no other arrays
+ * Norms are of h' before it is rounded; sums are fp32, and gate * b' is an fp32 number before scale is.  16-byte aligned, strides multiples of 8 (codes: of 16), at
+ * least `width` and at most 2^29; nothing behind a row's `width` elements is written, and what is read there, up to the next 16 bytes' end, may be anything.  h_out may be h, x may be block, of equal strides; no other arrays
  * may overlap.  Tokens do not affect each other; results do not depend on T.  Allocates nothing; may be captured in a HIP graph.
  */
 int32_t slora_norm_apply(const slora_norm *norm, int32_t T, const void *h, int64_t h_stride, const void *block, int64_t block_stride, const void *gate,

@@ -362,8 +362,9 @@ __device__ __forceinline__ int64_t row_number(int waves, int wave)
 }
 
 // One row for the workgroup, or (waves == 1) one for each of its wavefronts.
-// Bound: HBM where there are rows enough (8192 rows of 8192, a norm behind the block and a gate by channel, 537 MB: 97 us = 5.5 TB/s, a copy reaches 5.05; 2048
-// of 4096 14.9 us = 4.5 TB/s); below, the chain of two loads, two to four reductions and a store (777 rows of 5003 in fp32, gate by token: 15 us = 3.6 TB/s), and the launch (one row 6.5 us).
+// Bound: HBM where there are rows enough (8192 rows of 8192, a norm behind the block and a gate by channel, 537 MB: 97 us = 5.5 TB/s, a copy reaches 5.05; from memory 2048
+// of 4096 15.5 us = 4.3 TB/s, 12.6 where they are in the memory-side cache); below, the chain of two loads, two to four reductions and a store (777 rows of 5003 in fp32, gate by token: 19.6 us from
+// memory = 2.8 TB/s, 15 in that cache), and the launch (one row 6.1 - 7.5 us, 3.4 in the kernel).
 template <int DT, bool H32, int P, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void norm_kernel(NormArgs a, int waves)
 {

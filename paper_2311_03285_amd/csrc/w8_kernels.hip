@@ -94,7 +94,7 @@ __device__ __forceinline__ void lds_barrier()
 // in turn and are added up in LDS.
 // Weights of any size are loaded without a place in the caches: of a model whose layers take turns they are never there.  us with / without a place: 16 tokens, two of 20480 of 5120,
 // weights that are in no cache 43.9 / 39.8, three of 4096 of 4096 13.5 / 12.7; where all the weights that take turns are 200 MB 31.4 / 38.7 and 10.2 / 12.3.
-// Bound: HBM and the time to fill it: four of 4096 of 4096, one token 11.3 us = 5.9 TB/s; two of 20480 of 5120, one token 32 us = 6.5 TB/s, 16 tokens 39 us.  With more
+// Bound: HBM and the time to fill it: four of 4096 of 4096, one token 12.4 us from memory = 5.4 TB/s, 11.4 where 200 MB of them take turns; two of 20480 of 5120, one token 32 us = 6.5 TB/s, 16 tokens 39 us.  With more
 // tokens every 16 outputs read all of x again: two of 20480 of 5120, 32 tokens 81 us with one tile, 55 with two, 42 from LDS below.
 constexpr int kFewWaves = 8, kFewTokens = 16;
 template <int RT, int Y>

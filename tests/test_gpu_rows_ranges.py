@@ -54,7 +54,8 @@ def gates(dtype):
     t = DTYPES[dtype][1]
     bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(t)
     bits = bits[(bits.abs() >= 2.0 ** -20) & (bits.abs() <= 256)]
-    more = torch.tensor([0.0, -0.0, 1e3, -1e3, 6e4, -6e4] + ([1e20, -1e20, 3e38, -3e38] if dtype == "bf16" else []), dtype=torch.float32).to(t)
+    most = torch.finfo(t).max
+    more = torch.tensor([0.0, -0.0, 1e3, -1e3, 6e4, -6e4, most, -most] + ([1e20, -1e20, 3e38, -3e38] if dtype == "bf16" else []), dtype=torch.float32).to(t)
     return torch.cat([bits, more])
 
 
