@@ -556,7 +556,8 @@ int32_t slora_norm_apply(const slora_norm *norm, int32_t T, const void *h, int64
 /*
  * T rows of v = x (act == SLORA_ACT_NONE, gate NULL), or v = act(gate) * x, in 16 bits (y), in 8 bits (codes, scales), or both; what is NULL is not
  * wanted.  silu(g) = g / (1 + exp(-g)); gelu(g) = g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2; v is off by at most
- * 12 * 2^-24 of itself (or 2^-142) before it is rounded, also where silu(g) or gelu(g) alone is below fp32's range.  x, gate, y: of `dtype`.
+ * 12 * 2^-24 of itself (or 2^-142) before it is rounded, also where silu(g) or gelu(g) alone is below fp32's range; with gates below 2^-126, 2^-15 of itself.
+ * x, gate, y: of `dtype`.
  * 1 <= width <= SLORA_W8_MAX_WIDTH.  Arrays, strides, overlaps (y may be x or gate), asynchrony as for slora_norm_apply.
  * Runs on the HIP device that is current.
  */

@@ -50,13 +50,13 @@ def test_large_rows_with_an_eps(layer):
 
 
 def gates(dtype):
-    """every 16-bit number from 2^-20 to 256, of both signs, and some beyond"""
+    """every 16-bit number from 2^-126 (all of binary16's) to 256, of both signs, and some beyond"""
     t = DTYPES[dtype][1]
-    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(t)
-    bits = bits[(bits.abs() >= 2.0 ** -20) & (bits.abs() <= 256)]
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(t).float()
+    bits = bits[(bits.abs() >= 2.0 ** -126) & (bits.abs() <= 256)]
     most = torch.finfo(t).max
     more = torch.tensor([0.0, -0.0, 1e3, -1e3, 6e4, -6e4, most, -most] + ([1e20, -1e20, 3e38, -3e38] if dtype == "bf16" else []), dtype=torch.float32).to(t)
-    return torch.cat([bits, more])
+    return torch.cat([bits.to(t), more])
 
 
 @pytest.mark.parametrize("kind", [slora.ACT_SILU, slora.ACT_GELU])
@@ -64,7 +64,7 @@ def gates(dtype):
 def test_gates_of_every_size(dtype, kind, size):
     """x act(g) to 12 half-steps of fp32 (E each) before it is rounded, however small act(g) is; E are counted as: the exponential 2 and its argument's own roundings (of
     |r| <= 1, four at most, 2^-25 each times ln 2) 1.4, both once more halved in 1 + z; that sum 1, its reciprocal 2, three products 3: 3.4 + 1.7 + 1 + 2 + 3 < 12.
-    x 2^n below 2^-126 is off by 2^-150 at most, times at most |g| < 2^8 where the result is not 0.  Products of 0 and results beyond the type's range are left out."""
+    x 2^n below 2^-126 is off by 2^-150 at most, times at most |g| < 2^8 where the result is not 0; g / (1 + z) between 2^-127 and 2^-126 by one half-step more.  Products of 0 and results beyond the type's range are left out."""
     lib, t = DTYPES[dtype]
     g = gates(dtype)
     width = -(-len(g) // 8) * 8
@@ -114,3 +114,15 @@ def test_what_is_behind_a_row_changes_nothing_in_it(width, kind):
         out.append((y[:, :width], codes[:, :width], scales))
     for other in out[1:]:
         assert all(torch.equal(a, b) for a, b in zip(out[0], other))
+
+
+@pytest.mark.parametrize("kind", [slora.ACT_SILU, slora.ACT_GELU])
+def test_gates_below_the_normal_numbers(kind):
+    """act(g) is g / 2 there, which as an fp32 number is off by 2^-150: 2^-15 of itself at most for bfloat16's least, 2^-133; x may be large"""
+    g = torch.arange(1, 128, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    gate = torch.cat([g, -g, g[:2]]).reshape(1, 256).cuda()
+    x, y = torch.full((1, 256), 2.0 ** 110, dtype=torch.bfloat16, device="cuda"), torch.empty((1, 256), dtype=torch.bfloat16, device="cuda")
+    slora.w8_quantize(1, 256, slora.BF16, kind, x.data_ptr(), 256, gate.data_ptr(), 256, y.data_ptr(), 256)
+    torch.cuda.synchronize()
+    ref = gate.double().cpu().numpy() / 2 * 2.0 ** 110
+    du.within(y, ref, 2.0 ** -15 * np.abs(ref))
